@@ -93,7 +93,7 @@ def draw(rng):
         B = _log(rng, 1, 16)
         while B > 1 and (B * Nq * Nk * Hq * D > most or B * Nk * Hkv * D > 1 << 25):
             B -= 1
-        while B * Nq * Nk * Hq * D > most:
+        while B * Nq * Nk * Hq * D > most or B * Nq * Hq * D > 1 << 25:
             Nq = (Nq + 1) // 2
         return dict(kind=kind, B=B, Nq=Nq, Nk=Nk, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype, ragged=rng.random() < 0.4,
                     drop=rng.choice([0.0, 0.0, 0.1]))
