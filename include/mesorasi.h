@@ -53,7 +53,10 @@ enum {
     MESORASI_EWORKSPACE = -4     /* workspace NULL or smaller than the matching *_workspace() size */
 };
 
-enum { MESORASI_F32 = 0, MESORASI_BF16 = 1 };
+enum { MESORASI_F32 = 0, MESORASI_BF16 = 1, MESORASI_I8 = 2 /* rows of mesorasi_linear_i8 only */ };
+
+/* Activations of mesorasi_group_norm. */
+enum { MESORASI_ACT_NONE = 0, MESORASI_ACT_RELU = 1, MESORASI_ACT_SILU = 2, MESORASI_ACT_GELU = 3 };
 
 /* Limits (MESORASI_EUNSUPPORTED beyond them). */
 #define MESORASI_MAX_N_FPS 65536     /* points per cloud for FPS */
@@ -62,6 +65,11 @@ enum { MESORASI_F32 = 0, MESORASI_BF16 = 1 };
 #define MESORASI_MAX_C_KNN 128       /* kNN feature width */
 #define MESORASI_MAX_LAYERS 8        /* MLP depth */
 #define MESORASI_MAX_WIDTH 4096      /* MLP layer width */
+#define MESORASI_MAX_WIDTH_I8 65536  /* inputs or outputs of an 8-bit product (its sums stay in 32 bits) */
+#define MESORASI_MAX_C_NORM 65536    /* channels of a group norm */
+#define MESORASI_MAX_D_ATTN 128      /* channels of an attention head */
+#define MESORASI_MAX_D_ROTARY 1024   /* channels of a rotated head */
+#define MESORASI_MAX_AXES 4          /* coordinates of rotary positions */
 
 int mesorasi_version(void);
 const char* mesorasi_strerror(int status);
@@ -509,6 +517,166 @@ int mesorasi_edgeconv_fold(const float* W, const float* b, int32_t C, int32_t C_
  * Errors: EINVAL for NULL count, NULL idx with n > 0, n < 0.
  */
 int mesorasi_count_out_of_range(const int32_t* idx, int64_t n, int32_t bound, int32_t* count, void* stream);
+
+/*
+ * The operators of an attention level, which moves features from one set of
+ * points to another (another length) as mesorasi_interpolate3 does, with
+ * learned weights instead of inverse distances: group norm, 8-bit products,
+ * rotary positions and cross attention.  Rows are points, channels last.
+ */
+
+/*
+ * Group normalisation with an activation, channels last: the channels of
+ * each cloud fall into G groups of c = C / G neighbors, and over the valid
+ * points n < len_b of cloud b
+ *   mu = mean x, var = mean (x - mu)^2              (per cloud and group)
+ *   y  = act((x - mu) / sqrt(var + eps) * gamma + beta)
+ * with the statistics in fp32 or more.  Rows n >= len_b are not read and
+ * are written as 0.
+ *   x     [B, N, ld_x] of x_dtype (F32 or BF16), first C columns used
+ *   lens  [B] int32 or NULL (all N); a value outside [0, N] is taken as the
+ *         nearest of the two
+ *   gamma, beta [C] float32, nullable (1 and 0)
+ *   act   MESORASI_ACT_*: none, max(y, 0), y / (1 + exp(-y)), or
+ *         y (1 + erf(y / sqrt 2)) / 2
+ *   y     [B, N, ld_y] of y_dtype (F32 or BF16)
+ *   ws    at least mesorasi_group_norm_workspace() bytes, 16-byte aligned
+ *         (NULL allowed when that size is 0; any contents on entry); calls
+ *         that overlap in time need separate workspaces
+ * Errors: EINVAL for NULL x/y, sizes < 0, C < 1, G < 1, C % G != 0, ld < C,
+ *         an unknown act, eps negative or not finite, a misaligned ws;
+ *         EUNSUPPORTED for an unknown dtype, C > MESORASI_MAX_C_NORM, N or
+ *         B > 2^31 - 1, or more work than one launch holds; EWORKSPACE when
+ *         ws is too small.
+ */
+int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype, int64_t B, int64_t N, int32_t C, int32_t G,
+                        const int32_t* lens, const float* gamma, const float* beta, float eps, int32_t act, void* y,
+                        int64_t ld_y, int32_t y_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for mesorasi_group_norm with these sizes (0 when none is
+ * needed, and for invalid sizes). */
+size_t mesorasi_group_norm_workspace(int64_t B, int64_t N, int32_t C, int32_t G, int32_t x_dtype);
+
+/*
+ * Rows brought to 8 bits, one scale for each row:
+ *   a = max(max_c |x_c|, 2^-100), scale = fl32(a / 127), r = fl32(127 / a)
+ *   q_c = rint(fl32(x_c r))         (ties to even; in [-127, 127])
+ * A row that holds an infinity or a NaN has scale NaN and q = 0, so that a
+ * product of it is NaN.  Also lays out the weights of mesorasi_linear_i8
+ * (rows = output channels).
+ *   x     [rows, ld_x] of x_dtype (F32 or BF16), first C columns used
+ *   q     [rows, ld_q] int8 out, 16-byte aligned, ld_q a multiple of 16;
+ *         columns C .. up to the next multiple of 16 are written as 0
+ *   scale [rows] float32 out
+ * Errors: EINVAL for NULL pointers, rows < 0, C < 1, ld_x < C, ld_q < C or
+ *         not a multiple of 16, a misaligned q; EUNSUPPORTED for an unknown
+ *         dtype, C > MESORASI_MAX_WIDTH_I8 or rows > 2^31 - 1.
+ */
+int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype, int64_t rows, int32_t C, int8_t* q,
+                         int64_t ld_q, float* scale, void* stream);
+
+/*
+ * A layer's product in 8-bit integers with a scale for each row and each
+ * output channel, the 8-bit sibling of a mesorasi_pointwise_mlp layer:
+ *   y[r, o] = phi((float(sum_c xq[r, c] W[o, c]) x_scale[r]) w_scale[o] + bias[o])
+ * with the sum exact in 32-bit integers, phi = ReLU when relu != 0 (a NaN
+ * stays NaN).
+ *   x_dtype I8: x [rows, ld_x] int8 as mesorasi_quantize_i8 lays it out
+ *         (16-byte aligned, ld_x a multiple of 16; the columns up to the next
+ *         multiple of 16 are read, and multiplied by W's, which are 0),
+ *         x_scale [rows] float32.
+ *         F32 / BF16: x is brought to 8 bits by mesorasi_quantize_i8's rule
+ *         within the call; x_scale must be NULL.
+ *   W     [c_out, ld_w] int8 as mesorasi_quantize_i8 lays it out: 16-byte
+ *         aligned, ld_w a multiple of 16, columns c_in .. up to the next
+ *         multiple of 16 hold 0;  w_scale [c_out] float32
+ *   bias  [c_out] float32, nullable
+ *   y     [rows, ld_y] of y_dtype (F32 or BF16)
+ *   ws    at least mesorasi_linear_i8_workspace() bytes, 16-byte aligned
+ *         (NULL allowed when that size is 0; any contents on entry); calls
+ *         that overlap in time need separate workspaces
+ * Errors: EINVAL for NULL x/W/w_scale/y, rows < 0, c_in < 1, c_out < 1,
+ *         ld < width, an ld_w (or an I8 ld_x) that is no multiple of 16, a
+ *         misaligned W, ws or I8 x, x_scale missing (I8) or given
+ *         (F32, BF16); EUNSUPPORTED for an unknown dtype, a width above
+ *         MESORASI_MAX_WIDTH_I8 or rows > 2^31 - 1; EWORKSPACE when ws is too
+ *         small.
+ */
+int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, const float* x_scale, int64_t rows, int32_t c_in,
+                       const int8_t* W, int64_t ld_w, const float* w_scale, const float* bias, int32_t c_out,
+                       int32_t relu, void* y, int64_t ld_y, int32_t y_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for mesorasi_linear_i8 with these arguments (0 when none
+ * is needed, and for invalid ones). */
+size_t mesorasi_linear_i8_workspace(int64_t rows, int32_t c_in, int32_t c_out, int32_t x_dtype);
+
+/*
+ * Rotary positions with several axes: feature pairs of every head turn by
+ * angles of the row's coordinates (x, y, z of a point; time, height, width),
+ * so that products of rotated rows depend on coordinate differences.  The
+ * P = sum(sections) pairs are split over the axes in order: axis a turns the
+ * next sections[a] of them; pair j of axis a, (u, v), becomes
+ *   (u cos t - v sin t, u sin t + v cos t),  t = pos[r, a] freq[j]
+ * with t formed and reduced by 2 pi in 64 bits.  Pair j holds channels
+ * (j, j + P) of a head, or (2 j, 2 j + 1) when interleaved != 0; channels
+ * from 2 P on are copied.
+ *   x     [rows, ld_x] of dtype (F32 or BF16): H heads of D channels each, the
+ *         same angles for every head
+ *   pos   [rows, ld_pos] float32 (first n_axes columns)
+ *   sections host array [n_axes], each >= 0
+ *   freq  [P] float32
+ *   y     [rows, ld_y] of dtype; may be x itself when ld_y == ld_x
+ * Errors: EINVAL for NULL pointers, rows < 0, H < 1, D < 1, ld < width, a
+ *         negative section, P < 1, 2 P > D, y == x with another leading
+ *         dimension; EUNSUPPORTED for an unknown dtype, n_axes outside
+ *         [1, MESORASI_MAX_AXES], D > MESORASI_MAX_D_ROTARY, H > 65536 or
+ *         rows > 2^31 - 1.
+ */
+int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t H, int32_t D, const float* pos,
+                    int64_t ld_pos, int32_t n_axes, const int32_t* sections, const float* freq, int32_t interleaved,
+                    void* y, int64_t ld_y, void* stream);
+
+/*
+ * Cross attention: every query point i of cloud b attends to the points of
+ * another set of another length,
+ *   s_ij = scale q_i . k_j,  p_ij = exp(s_ij - max_j s_ij),
+ *   o_i  = sum_j p_ij v_j / sum_j p_ij
+ * over the valid sources j: j < k_len[b] and k_mask[b, j] != 0.  Query head
+ * h reads source head h / (Hq / Hkv).  A query without any valid source (or
+ * whose every score is -infinity) gives 0; k and v rows that are not valid
+ * may hold anything, infinities and NaN included.  Maximum, sum and output
+ * are accumulated in fp32; the bf16 form rounds the weights p to bf16 before
+ * their product with v, the fp32 form keeps fp32 precision throughout.
+ *   q [B, Nq, Hq, D], k and v [B, Nk, Hkv, D], o [B, Nq, Hq, D], all of dtype
+ *         (F32 or BF16), each with strides in elements: *_bs between clouds,
+ *         *_ld between points, *_hs between heads; channels contiguous.  So
+ *         heads may lie side by side in a row or one after another, k and v may
+ *         be columns of one projection, and a set may be the filled part of a
+ *         longer buffer.  Input strides may be 0 (shared by clouds or heads).
+ *   k_len  [B] int32 or NULL (all Nk); a value outside [0, Nk] is taken as the
+ *         nearest of the two
+ *   k_mask [B, mask_ld] bytes or NULL (all valid)
+ *   ws    at least mesorasi_cross_attention_workspace() bytes, 16-byte aligned
+ *         (NULL allowed when that size is 0; any contents on entry); calls
+ *         that overlap in time need separate workspaces
+ * Errors: EINVAL for NULL q/k/v/o, sizes < 0, Hq < 1, Hkv < 1,
+ *         Hq % Hkv != 0, D < 1, a negative stride, an output stride < D (over
+ *         more than one cloud, point or head), mask_ld < Nk with a mask and
+ *         more than one cloud, a scale that is not finite, a misaligned ws;  EUNSUPPORTED for an unknown dtype,
+ *         D > MESORASI_MAX_D_ATTN, Nq (Hq / Hkv) or Nk > 2^31 - 1024, or more
+ *         work than one launch holds;  EWORKSPACE when ws is too small.
+ *         Nk == 0 is valid: every output is 0.
+ */
+int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_ld, int64_t q_hs, const void* k, int64_t k_bs,
+                             int64_t k_ld, int64_t k_hs, const void* v, int64_t v_bs, int64_t v_ld, int64_t v_hs,
+                             int32_t dtype, int64_t B, int64_t Nq, int64_t Nk, int32_t Hq, int32_t Hkv, int32_t D,
+                             float scale, const int32_t* k_len, const uint8_t* k_mask, int64_t mask_ld, void* o,
+                             int64_t o_bs, int64_t o_ld, int64_t o_hs, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for mesorasi_cross_attention with these sizes (0 when none
+ * is needed, and for invalid ones). */
+size_t mesorasi_cross_attention_workspace(int64_t B, int64_t Nq, int64_t Nk, int32_t Hq, int32_t Hkv, int32_t D,
+                                          int32_t dtype);
 
 #ifdef __cplusplus
 }

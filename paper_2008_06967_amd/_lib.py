@@ -15,7 +15,8 @@ LIB_PATH = os.environ.get("MESORASI_LIBRARY") or os.path.join(HERE, "libmesorasi
 
 OK, EINVAL, EUNSUPPORTED, EHIP, EWORKSPACE = 0, -1, -2, -3, -4
 NOALLOC_WS_BYTES = 32 << 20    # MESORASI_NOALLOC_WS_BYTES: the allocation-free MLP's fixed scratch
-F32, BF16 = 0, 1
+F32, BF16, I8 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 _i64, _i32, _u32, _p, _f = ctypes.c_int64, ctypes.c_int32, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_float
 _size = ctypes.c_size_t
@@ -61,6 +62,18 @@ SIGNATURES = {
     "mesorasi_count_out_of_range": (ctypes.c_int, [_p, _i64, _i32, _p, _p]),
     "mesorasi_aggregate_mlp": (ctypes.c_int, [_p, _p, _i64, _p, _p, _i64, _i64, _i64, _i32, _i32, _i32, _p, _p, _p,
                                               _u32, _p, _i64, _p, _i64, _p]),
+    "mesorasi_group_norm": (ctypes.c_int, [_p, _i64, _i32, _i64, _i64, _i32, _i32, _p, _p, _p, _f, _i32, _p, _i64,
+                                           _i32, _p, _size, _p]),
+    "mesorasi_group_norm_workspace": (_size, [_i64, _i64, _i32, _i32, _i32]),
+    "mesorasi_quantize_i8": (ctypes.c_int, [_p, _i64, _i32, _i64, _i32, _p, _i64, _p, _p]),
+    "mesorasi_linear_i8": (ctypes.c_int, [_p, _i64, _i32, _p, _i64, _i32, _p, _i64, _p, _p, _i32, _i32, _p, _i64,
+                                          _i32, _p, _size, _p]),
+    "mesorasi_linear_i8_workspace": (_size, [_i64, _i32, _i32, _i32]),
+    "mesorasi_rotary": (ctypes.c_int, [_p, _i64, _i32, _i64, _i32, _i32, _p, _i64, _i32, _p, _p, _i32, _p, _i64, _p]),
+    "mesorasi_cross_attention": (ctypes.c_int, [_p, _i64, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _i64,
+                                                _i32, _i64, _i64, _i64, _i32, _i32, _i32, _f, _p, _p, _i64, _p, _i64,
+                                                _i64, _i64, _p, _size, _p]),
+    "mesorasi_cross_attention_workspace": (_size, [_i64, _i64, _i64, _i32, _i32, _i32, _i32]),
 }
 
 _lib = None

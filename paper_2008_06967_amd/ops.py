@@ -13,7 +13,7 @@ import math
 import torch
 
 from . import _lib
-from ._lib import F32, BF16, check
+from ._lib import F32, BF16, I8, check
 
 _vp = ctypes.c_void_p
 
@@ -526,3 +526,318 @@ def count_out_of_range(idx: torch.Tensor, bound: int, out: torch.Tensor | None =
     check(_lib.lib().mesorasi_count_out_of_range(idx.data_ptr(), idx.numel(), int(bound), count.data_ptr(),
                                                  _stream()), "count_out_of_range")
     return count
+
+
+# ---------------------------------------------------------------------------
+# the operators of an attention level
+# ---------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_ACTS = {"none": _lib.ACT_NONE, "relu": _lib.ACT_RELU, "silu": _lib.ACT_SILU, "gelu": _lib.ACT_GELU}
+
+
+def _require(cond, msg: str):
+    if not cond:
+        raise ValueError(msg)
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return dt
+
+
+def _like(t, x: torch.Tensor, name: str, dtype, shape):
+    """t (may be None) is a contiguous tensor of this dtype and shape on x's device."""
+    if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()
+                              and t.device == x.device):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {x.device}")
+
+
+def _call(x: torch.Tensor, where: str, *args):
+    """The entry point `where` on x's device, on that device's current stream."""
+    dev = x.device
+    if dev.type != "cuda":
+        raise ValueError(f"{where}: tensors must be on a GPU, not on {dev}")
+    fn = getattr(_lib.lib(), "mesorasi_" + where)
+    if dev.index == torch.cuda.current_device():
+        check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
+    else:
+        with torch.cuda.device(dev):
+            check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
+
+
+def _workspace(x: torch.Tensor, need: int, ws):
+    """(pointer, bytes, tensor) of the caller's workspace, or of a new one
+    when it is missing or too small."""
+    if not need:
+        return None, 0, None
+    _require(ws is None or (ws.device == x.device and ws.dtype == torch.uint8 and ws.is_contiguous()),
+             f"ws must be a contiguous uint8 tensor on {x.device}")
+    if ws is None or ws.numel() < need:
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return ws.data_ptr(), ws.numel(), ws
+
+
+def _ld(t: torch.Tensor, name: str):
+    """(pointer, leading dimension) of rows, which must collapse; the stride
+    of a single row is not used."""
+    _require(t.dim() >= 2 and (t.shape[-1] <= 1 or t.stride(-1) == 1), f"{name}'s last dimension must be contiguous")
+    n, ld = 1, None
+    for d in range(t.dim() - 2, -1, -1):
+        if t.shape[d] == 1:
+            continue
+        if ld is None:
+            ld = t.stride(d)
+        _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
+        n *= t.shape[d]
+    return t.data_ptr(), t.shape[-1] if ld is None or n == 0 else ld
+
+
+def group_norm_workspace_bytes(B: int, N: int, C: int, G: int, dtype: int = F32) -> int:
+    return int(_lib.lib().mesorasi_group_norm_workspace(B, N, C, G, dtype))
+
+
+def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None,
+               eps: float = 1e-5, act: str = "none", lens: torch.Tensor | None = None,
+               out: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Group norm over each cloud's valid points with an activation ("none",
+    "relu", "silu", "gelu").  x [B, N, C] float32 or bfloat16; gamma, beta
+    [C] float32; lens [B] int32 (rows from lens[b] on are not read and come
+    out 0).  out: like x, or of the other type (see the C header)."""
+    _require(x.dim() == 3, "x must be [B, N, C]")
+    _require(act in _ACTS, f"act must be one of {sorted(_ACTS)}")
+    B, N, C = x.shape
+    dt = _dtype(x, "x")
+    _like(gamma, x, "gamma", torch.float32, (C,))
+    _like(beta, x, "beta", torch.float32, (C,))
+    _like(lens, x, "lens", torch.int32, (B,))
+    if out is None:
+        out = torch.empty((B, N, C), dtype=x.dtype, device=x.device)
+    else:
+        _require(tuple(out.shape) == (B, N, C) and out.device == x.device, "out must have x's shape and device")
+    px, ldx = _ld(x, "x")
+    py, ldy = _ld(out, "out")
+    wp, wn, ws = _workspace(x, group_norm_workspace_bytes(B, N, C, groups, dt), ws)
+    _call(x, "group_norm", px, ldx, dt, B, N, C, groups, _ptr(lens), _ptr(gamma), _ptr(beta), eps, _ACTS[act], py, ldy,
+          _dtype(out, "out"), wp, wn)
+    return out
+
+
+def quantize_int8(x: torch.Tensor, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """Rows in 8 bits with a scale each: (q, scale) of x [..., C] float32 or
+    bfloat16.  q [..., C] int8 has rows a multiple of 16 bytes apart, as
+    linear_int8 reads them."""
+    dt = _dtype(x, "x")
+    px, ldx = _ld(x, "x")
+    C, lead = x.shape[-1], tuple(x.shape[:-1])
+    rows = math.prod(lead)
+    if out is None:
+        out = torch.empty(lead + ((C + 15) // 16 * 16,), dtype=torch.int8, device=x.device)[..., :C]
+    else:
+        _require(out.dtype == torch.int8 and out.shape == x.shape and out.device == x.device,
+                 "out must be int8 of x's shape, on x's device")
+    if scale is None:
+        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    else:
+        _like(scale, x, "scale", torch.float32, lead)
+    pq, ldq = _ld_int8(out, "out")
+    _call(x, "quantize_i8", px, ldx, dt, rows, C, pq, ldq, scale.data_ptr())
+    return out, scale
+
+
+def _ld_int8(t: torch.Tensor, name: str):
+    """_ld() of 8-bit rows: a single row's leading dimension is its width
+    rounded up to 16, within the storage."""
+    p, ld = _ld(t, name)
+    C = t.shape[-1]
+    pad = (C + 15) // 16 * 16
+    if ld == C and ld % 16 and t.numel() == C:
+        ld = pad
+    if t.numel() and ld % 16 == 0:
+        have = t.untyped_storage().nbytes() - t.storage_offset()
+        _require((t.numel() // C - 1) * ld + pad <= have,
+                 f"{name}'s last row must be followed by its padding to 16 bytes")
+    return p, ld
+
+
+def int8_rows(q: torch.Tensor) -> torch.Tensor:
+    """int8 rows [..., C] laid out as linear_int8 reads them: a multiple of
+    16 bytes apart, zeros behind each."""
+    _require(q.dtype == torch.int8, "q must be int8")
+    C = q.shape[-1]
+    t = torch.zeros(tuple(q.shape[:-1]) + ((C + 15) // 16 * 16,), dtype=torch.int8, device=q.device)
+    t[..., :C] = q
+    return t[..., :C]
+
+
+class Int8Params:
+    """One layer's weights in 8 bits on the device, laid out for
+    linear_int8: Wq [C_out, C_in] int8, w_scale [C_out] float32 (channel o's
+    weights are Wq[o] w_scale[o]), bias [C_out] float32 or None."""
+
+    def __init__(self, Wq, w_scale, bias=None, device="cuda"):
+        Wq, w_scale = torch.as_tensor(Wq), torch.as_tensor(w_scale)
+        _require(Wq.dtype == torch.int8 and Wq.dim() == 2, "Wq must be int8 [C_out, C_in]")
+        self.c_out, self.c_in = int(Wq.shape[0]), int(Wq.shape[1])
+        _require(w_scale.numel() == self.c_out, "w_scale must hold one scale for each output channel")
+        if Wq.is_cuda:
+            device = Wq.device
+        self.W = int8_rows(Wq.to(device))
+        self.ld = (self.c_in + 15) // 16 * 16
+        self.w_scale = w_scale.to(device=device, dtype=torch.float32).reshape(-1).contiguous()
+        self.bias = None
+        if bias is not None:
+            self.bias = torch.as_tensor(bias).to(device=device, dtype=torch.float32).reshape(-1).contiguous()
+            _require(self.bias.numel() == self.c_out, "bias must hold one value for each output channel")
+
+    @classmethod
+    def from_float(cls, W, bias=None, device="cuda"):
+        """Float weights [C_out, C_in] brought to 8 bits by quantize_int8's
+        rule, a scale for each output channel."""
+        W = torch.as_tensor(W, dtype=torch.float32)
+        q, s = quantize_int8((W if W.is_cuda else W.to(device)).contiguous())
+        return cls(q, s, bias)
+
+
+def linear_int8_workspace_bytes(rows: int, p: Int8Params, dtype: int = F32) -> int:
+    return int(_lib.lib().mesorasi_linear_i8_workspace(rows, p.c_in, p.c_out, dtype))
+
+
+def linear_int8(x: torch.Tensor, p: Int8Params, x_scale: torch.Tensor | None = None, relu: bool = False,
+                out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+                ws: torch.Tensor | None = None):
+    """A layer's product in 8-bit integers.  x [..., C_in] float32 or
+    bfloat16 (brought to 8 bits within the call), or int8 rows of
+    quantize_int8() with their x_scale.  out_dtype: float32 (the default) or
+    bfloat16."""
+    int8 = x.dtype == torch.int8
+    dt = I8 if int8 else _dtype(x, "x")
+    if x.shape[-1] != p.c_in:
+        raise ValueError(f"x has {x.shape[-1]} columns, the weights {p.c_in}")
+    _require(p.W.device == x.device, "the weights are on another device than x")
+    lead = tuple(x.shape[:-1])
+    rows = math.prod(lead)
+    _require(int8 == (x_scale is not None), "x_scale goes with int8 rows, and only with them")
+    if int8:
+        _like(x_scale, x, "x_scale", torch.float32, lead)
+        px, ldx = _ld_int8(x, "x")
+    else:
+        px, ldx = _ld(x, "x")
+    if out is None:
+        out = torch.empty(lead + (p.c_out,), dtype=out_dtype or torch.float32, device=x.device)
+    else:
+        _require(tuple(out.shape) == lead + (p.c_out,) and out.device == x.device
+                 and out_dtype in (None, out.dtype), "out must be [..., C_out] of out_dtype on x's device")
+    py, ldy = _ld(out, "out")
+    wp, wn, ws = _workspace(x, linear_int8_workspace_bytes(rows, p, dt), ws)
+    _call(x, "linear_i8", px, ldx, dt, _ptr(x_scale), rows, p.c_in, p.W.data_ptr(), p.ld, p.w_scale.data_ptr(),
+          _ptr(p.bias), p.c_out, 1 if relu else 0, py, ldy, _dtype(out, "out"), wp, wn)
+    return out
+
+
+class RotaryParams:
+    """The angles of rotary positions: sections[a] pairs of a head turn by
+    coordinate a, pair i of a section of s by freq = scale base^(-i / s)
+    radians per unit, or by the given freq [sum(sections)]."""
+
+    def __init__(self, sections, freq=None, base: float = 10000.0, scale: float = 1.0, interleaved: bool = False,
+                 device="cuda"):
+        self.sections = [int(s) for s in sections]
+        self.interleaved = bool(interleaved)
+        if freq is None:
+            freq = torch.tensor([scale * base ** (-i / s) for s in self.sections for i in range(s)],
+                                dtype=torch.float32)
+        freq = torch.as_tensor(freq, dtype=torch.float32)
+        self.freq = (freq if freq.is_cuda else freq.to(device)).reshape(-1).contiguous()
+        _require(1 <= len(self.sections) <= 4 and min(self.sections) >= 0, "1 to 4 sections of 0 or more pairs")
+        _require(self.freq.numel() == sum(self.sections), "freq must hold one value for each pair")
+        self._sections_c = (ctypes.c_int32 * len(self.sections))(*self.sections)
+
+
+def rotary(x: torch.Tensor, pos: torch.Tensor, p: RotaryParams, out: torch.Tensor | None = None):
+    """Every head's feature pairs turned by the row's coordinates.  x [..., H,
+    D] float32 or bfloat16, heads side by side; pos [..., axes] float32.  out
+    may be x."""
+    dt = _dtype(x, "x")
+    _require(x.dim() >= 2, "x must be [..., H, D]")
+    H, D = x.shape[-2], x.shape[-1]
+    lead = tuple(x.shape[:-2])
+    if pos.dtype != torch.float32 or tuple(pos.shape) != lead + (len(p.sections),) or pos.device != x.device:
+        raise ValueError(f"pos must be float32 {list(lead) + [len(p.sections)]} on {x.device}")
+    _require(p.freq.device == x.device, "the frequencies are on another device than x")
+    if out is None:
+        out = torch.empty(lead + (H, D), dtype=x.dtype, device=x.device)
+    else:
+        _require(out.dtype == x.dtype and out.shape == x.shape and out.device == x.device, "out must be like x")
+    rows = math.prod(lead)
+    px, ldx = _heads(x, "x")
+    py, ldy = _heads(out, "out")
+    pp, ldp = _ld(pos if pos.dim() >= 2 else pos[None], "pos")
+    _call(x, "rotary", px, ldx, dt, rows, H, D, pp, ldp, len(p.sections), p._sections_c, p.freq.data_ptr(),
+          1 if p.interleaved else 0, py, ldy)
+    return out
+
+
+def _heads(t: torch.Tensor, name: str):
+    """(pointer, leading dimension) of [..., H, D] rows of heads side by side."""
+    H, D = t.shape[-2], t.shape[-1]
+    _require((D <= 1 or t.stride(-1) == 1) and (H <= 1 or t.stride(-2) == D), f"{name}'s heads must lie side by side")
+    n, ld = 1, None
+    for d in range(t.dim() - 3, -1, -1):
+        if t.shape[d] == 1:
+            continue
+        if ld is None:
+            ld = t.stride(d)
+        _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
+        n *= t.shape[d]
+    return t.data_ptr(), H * D if ld is None or n == 0 else ld
+
+
+def cross_attention_workspace_bytes(B: int, Nq: int, Nk: int, Hq: int, Hkv: int, D: int, dtype: int = F32) -> int:
+    return int(_lib.lib().mesorasi_cross_attention_workspace(B, Nq, Nk, Hq, Hkv, D, dtype))
+
+
+def _strides(t: torch.Tensor, name: str):
+    """Cloud, point and head strides; those of single entries are not used."""
+    D = t.shape[3]
+    _require(D <= 1 or t.stride(3) == 1, f"{name}'s channels must be contiguous")
+    return tuple(t.stride(d) if t.shape[d] > 1 else 0 for d in range(3))
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: torch.Tensor | None = None,
+                    k_mask: torch.Tensor | None = None, scale: float | None = None,
+                    out: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Every query point over the points of another set.  q [B, Nq, Hq, D];
+    k, v [B, Nk, Hkv, D], Hq a multiple of Hkv; float32 or bfloat16, any
+    strides with contiguous channels (views of one projection, a head-major
+    layout transposed, the filled part of a longer buffer).  k_len [B] int32:
+    sources from k_len[b] on are not valid; k_mask [B, Nk] bool: only the True
+    ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
+    unless given.  out: like q (its strides may differ)."""
+    _require(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
+    B, Nq, Hq, D = q.shape
+    Nk, Hkv = k.shape[1], k.shape[2]
+    _require(k.shape[0] == B and k.shape[3] == D, "q, k and v must agree in B and D")
+    _require(k.dtype == q.dtype and v.dtype == q.dtype and k.device == q.device and v.device == q.device,
+             "q, k and v must have one type and device")
+    dt = _dtype(q, "q")
+    _like(k_len, q, "k_len", torch.int32, (B,))
+    mask_ld = 0
+    if k_mask is not None:
+        if not (k_mask.dtype in (torch.bool, torch.uint8) and tuple(k_mask.shape) == (B, Nk)
+                and k_mask.device == q.device and (Nk <= 1 or k_mask.stride(1) == 1)):
+            raise ValueError(f"k_mask must be bool [{B}, {Nk}] with contiguous rows on {q.device}")
+        mask_ld = k_mask.stride(0) if B > 1 else Nk
+    if scale is None:
+        scale = 1.0 / math.sqrt(D) if D else 1.0
+    if out is None:
+        out = torch.empty((B, Nq, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _require(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out must be like q")
+    wp, wn, ws = _workspace(q, cross_attention_workspace_bytes(B, Nq, Nk, Hq, Hkv, D, dt), ws)
+    _call(q, "cross_attention", q.data_ptr(), *_strides(q, "q"), k.data_ptr(), *_strides(k, "k"), v.data_ptr(),
+          *_strides(v, "v"), dt, B, Nq, Nk, Hq, Hkv, D, scale, _ptr(k_len), _ptr(k_mask), mask_ld, out.data_ptr(),
+          *_strides(out, "out"), wp, wn)
+    return out

@@ -356,3 +356,116 @@ def test_aggregate_mlp_validation():
     d3, _, _ = _mlp_args([65, 64, 64])
     assert st(f, FAKE, FAKE, 62, FAKE, FAKE, 2, 100, 10, 8, 62, 2, d3, W, b, 7, FAKE, 128, NULL, 0, NULL) == \
         _lib.EUNSUPPORTED                                            # C not a multiple of 4
+
+
+def test_group_norm_validation():
+    L = _lib.lib()
+    f = "mesorasi_group_norm"
+
+    def args(x=FAKE, ldx=64, xd=0, B=2, N=100, C=64, G=8, eps=1e-5, act=1, y=FAKE, ldy=64, yd=0, ws=FAKE,
+             wn=1 << 30):
+        return x, ldx, xd, B, N, C, G, NULL, NULL, NULL, eps, act, y, ldy, yd, ws, wn, NULL
+
+    assert st(f, *args(x=NULL)) == _lib.EINVAL
+    assert st(f, *args(y=NULL)) == _lib.EINVAL
+    assert st(f, *args(B=-1)) == _lib.EINVAL
+    assert st(f, *args(N=-1)) == _lib.EINVAL
+    assert st(f, *args(C=0)) == _lib.EINVAL
+    assert st(f, *args(G=0)) == _lib.EINVAL
+    assert st(f, *args(G=7)) == _lib.EINVAL                    # C % G != 0
+    assert st(f, *args(ldx=63)) == _lib.EINVAL
+    assert st(f, *args(ldy=63)) == _lib.EINVAL
+    assert st(f, *args(act=4)) == _lib.EINVAL
+    assert st(f, *args(eps=-1.0)) == _lib.EINVAL
+    assert st(f, *args(eps=float("nan"))) == _lib.EINVAL
+    assert st(f, *args(xd=2)) == _lib.EUNSUPPORTED             # 8-bit rows
+    assert st(f, *args(yd=5)) == _lib.EUNSUPPORTED
+    assert st(f, *args(C=1 << 17, ldx=1 << 17, ldy=1 << 17)) == _lib.EUNSUPPORTED
+    assert st(f, *args(N=1 << 31)) == _lib.EUNSUPPORTED
+    assert st(f, *args(B=1 << 31)) == _lib.EUNSUPPORTED
+    assert st(f, *args(x=NULL, y=NULL, B=0)) == _lib.OK        # no clouds
+    assert st(f, *args(x=NULL, y=NULL, N=0)) == _lib.OK        # no points
+    assert L.mesorasi_group_norm_workspace(2, 100, 64, 7, 0) == 0
+    st(f, *args(G=7))
+    assert b"G = 7" in L.mesorasi_last_error()
+
+
+def test_quantize_i8_validation():
+    f = "mesorasi_quantize_i8"
+
+    def args(x=FAKE, ldx=100, xd=0, rows=4, C=100, q=FAKE, ldq=112, s=FAKE):
+        return x, ldx, xd, rows, C, q, ldq, s, NULL
+
+    for bad in (dict(x=NULL), dict(q=NULL), dict(s=NULL), dict(rows=-1), dict(C=0), dict(ldx=99), dict(ldq=96),
+                dict(ldq=104), dict(q=ctypes.c_void_p(0x1008))):
+        assert st(f, *args(**bad)) == _lib.EINVAL, bad
+    for bad in (dict(xd=2), dict(xd=7), dict(C=65537, ldx=70000, ldq=70400), dict(rows=1 << 31)):
+        assert st(f, *args(**bad)) == _lib.EUNSUPPORTED, bad
+    assert st(f, *args(x=NULL, q=NULL, s=NULL, rows=0)) == _lib.OK
+
+
+def test_linear_i8_validation_and_workspace():
+    L = _lib.lib()
+    f = "mesorasi_linear_i8"
+
+    def args(x=FAKE, ldx=100, xd=0, xs=NULL, rows=3000, ci=100, W=FAKE, ldw=112, wsc=FAKE, co=50, y=FAKE, ldy=50,
+             yd=0, ws=FAKE, wn=1 << 30):
+        return x, ldx, xd, xs, rows, ci, W, ldw, wsc, NULL, co, 1, y, ldy, yd, ws, wn, NULL
+
+    odd = ctypes.c_void_p(0x1008)
+    for bad in (dict(x=NULL), dict(W=NULL), dict(wsc=NULL), dict(y=NULL), dict(rows=-1), dict(ci=0), dict(co=0),
+                dict(ldx=99), dict(ldw=96), dict(ldw=104), dict(ldy=49), dict(xs=FAKE), dict(xd=2, ldx=112),
+                dict(xd=2, xs=FAKE, ldx=100), dict(xd=2, xs=FAKE, ldx=112, x=odd), dict(W=odd), dict(ws=odd)):
+        assert st(f, *args(**bad)) == _lib.EINVAL, bad
+    for bad in (dict(xd=3), dict(yd=2), dict(ci=65537, ldx=70000, ldw=70400), dict(co=65537, ldy=70000),
+                dict(rows=1 << 31)):
+        assert st(f, *args(**bad)) == _lib.EUNSUPPORTED, bad
+    need = L.mesorasi_linear_i8_workspace(3000, 100, 50, 0)
+    assert need >= 3000 * (112 + 4)
+    assert st(f, *args(ws=NULL)) == _lib.EWORKSPACE
+    assert st(f, *args(wn=need - 1)) == _lib.EWORKSPACE
+    assert L.mesorasi_linear_i8_workspace(0, 100, 50, 0) == 0
+    assert st(f, *args(x=NULL, W=NULL, wsc=NULL, y=NULL, ws=NULL, rows=0)) == _lib.OK
+
+
+def test_rotary_validation():
+    L = _lib.lib()
+    f = "mesorasi_rotary"
+    S = (ctypes.c_int32 * 4)(10, 10, 10, 0)
+    other = ctypes.c_void_p(0x2000)
+
+    def args(x=FAKE, ldx=512, xd=0, rows=4, H=8, D=64, pos=FAKE, ldp=3, axes=3, sec=S, freq=FAKE, y=other, ldy=512):
+        return x, ldx, xd, rows, H, D, pos, ldp, axes, sec, freq, 0, y, ldy, NULL
+
+    neg, none = (ctypes.c_int32 * 3)(10, -1, 10), (ctypes.c_int32 * 3)(0, 0, 0)
+    huge = (ctypes.c_int32 * 3)(0x7fffffff, 0x7fffffff, 0x7fffffff)
+    for bad in (dict(x=NULL), dict(y=NULL), dict(pos=NULL), dict(sec=NULL), dict(freq=NULL), dict(rows=-1), dict(H=0),
+                dict(D=0), dict(D=58), dict(ldx=511), dict(ldy=511), dict(ldp=2), dict(sec=neg), dict(sec=none),
+                dict(sec=huge), dict(y=FAKE, ldy=520)):
+        assert st(f, *args(**bad)) == _lib.EINVAL, bad
+    for bad in (dict(xd=2), dict(axes=0), dict(axes=5), dict(D=1026, ldx=9000, ldy=9000), dict(rows=1 << 31)):
+        assert st(f, *args(**bad)) == _lib.EUNSUPPORTED, bad
+    assert st(f, *args(x=NULL, y=NULL, pos=NULL, freq=NULL, rows=0)) == _lib.OK
+    st(f, *args(D=58))
+    assert b"30 pairs" in L.mesorasi_last_error()
+
+
+def test_cross_attention_validation_and_workspace():
+    L = _lib.lib()
+    f = "mesorasi_cross_attention"
+
+    def args(q=FAKE, qs=(1024, 256, 64), k=FAKE, ks=(2048, 128, 64), v=FAKE, vs=(2048, 128, 64), dt=1, B=2, Nq=4,
+             Nk=16, Hq=4, Hkv=2, D=64, scale=0.125, mask=NULL, mld=0, o=FAKE, os=(1024, 256, 64), ws=FAKE, wn=1 << 30):
+        return (q, *qs, k, *ks, v, *vs, dt, B, Nq, Nk, Hq, Hkv, D, scale, NULL, mask, mld, o, *os, ws, wn, NULL)
+
+    for bad in (dict(q=NULL), dict(k=NULL), dict(v=NULL), dict(o=NULL), dict(B=-1), dict(Nq=-1), dict(Nk=-1),
+                dict(Hq=0), dict(Hkv=0), dict(Hkv=3), dict(D=0), dict(qs=(1024, -256, 64)), dict(ks=(-1, 128, 64)),
+                dict(vs=(2048, 128, -64)), dict(os=(1024, 63, 64)), dict(os=(1024, 256, 63)), dict(os=(0, 256, 64)),
+                dict(mask=FAKE, mld=15), dict(scale=float("inf")), dict(scale=float("nan"))):
+        assert st(f, *args(**bad)) == _lib.EINVAL, bad
+    for bad in (dict(dt=2), dict(D=129, os=(9999, 999, 199)), dict(Nk=1 << 31), dict(Nq=1 << 30)):
+        assert st(f, *args(**bad)) == _lib.EUNSUPPORTED, bad
+    assert st(f, *args(q=NULL, o=NULL, B=0)) == _lib.OK
+    assert st(f, *args(q=NULL, o=NULL, Nq=0)) == _lib.OK
+    assert L.mesorasi_cross_attention_workspace(2, 4, 16, 4, 3, 64, 1) == 0
+    assert L.mesorasi_cross_attention_workspace(2, -4, 16, 4, 2, 64, 1) == 0
