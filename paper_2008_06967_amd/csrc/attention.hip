@@ -8,6 +8,15 @@ namespace meso {
 
 namespace {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((address_space(3))) const char* lds_cptr;
+
+constexpr int kAtThreads = 256;
+
 struct AttnArgs {
     const void* q;
     const void* k;
@@ -19,6 +28,13 @@ struct AttnArgs {
     float scale;
     const int32_t* k_len;
     const uint8_t* k_mask;
+    // the launch
+    int rows;           // query rows of a cloud and source head: Nq (Hq / Hkv)
+    int row_tiles;      // workgroups over them
+    int splits;         // workgroups over the sources
+    int64_t blocks;     // pairs * row_tiles * splits
+    int per_xcd;
+    float* part;        // splits > 1: [pair, split, row, Dp] sums, then [pair, split, row, 2] maximum and sum
 };
 
 template <typename T>
@@ -92,6 +108,501 @@ __global__ __launch_bounds__(64) void attention_kernel(AttnArgs a, int64_t total
     }
 }
 
+
+// ---------------------------------------------------------------------------
+// bf16
+// ---------------------------------------------------------------------------
+
+__device__ const uint4 kAtZero[1] = {};
+
+// Slot of a 16-byte chunk in its row of CH chunks: rows that one read
+// touches together lie in different banks (the scores read one chunk of 16
+// rows, the transposed reads two chunks of 8 rows).
+template <int CH>
+__device__ __forceinline__ int at_swz(int row) {
+    const int top = (row >> 3) & 1;
+    if constexpr (CH == 16)
+        return ((row & 7) << 1) | top;
+    else if constexpr (CH == 8)
+        return (((row >> 1) & 3) << 1) | top;
+    else
+        return (((row >> 2) & 1) << 1) | top;
+}
+
+// 16 bytes from each lane's address to LDS at base + 16 lane.  The wait is
+// the caller's: at_wait_loads() before the barrier that publishes the tile.
+__device__ __forceinline__ void at_load_lds(const void* g, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(g)
+                 : "memory");
+}
+__device__ __forceinline__ void at_wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ float at_other_half(float v, float& lo) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    lo = __uint_as_float(r[0]);
+    return __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ uint32_t at_pack(float a, float b) {
+    bf16x2 v;
+    v[0] = static_cast<__bf16>(a);
+    v[1] = static_cast<__bf16>(b);
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// Valid sources among the 64 from j0 on.
+__device__ __forceinline__ uint64_t at_count_bits(int64_t j0, int64_t end) {
+    const int64_t r = end - j0;
+    return r >= 64 ? ~0ull : r <= 0 ? 0ull : (1ull << r) - 1;
+}
+
+// The product taken transposed, S^T = K Q^T and O^T = V^T P^T on
+// v_mfma_f32_32x32x16_bf16: a lane's 16 accumulators of a block of 32
+// sources belong to its own query (lane % 32), sources 8 (r / 4) + 4 (lane /
+// 32) + r % 4.  So the maximum and the sum of a query's weights stay in its
+// two lanes, and the weights, rounded to bf16 and packed, are the next
+// product's operand as they lie if its step t takes element e of lane half h
+// to be source 16 t + 8 (e / 4) + 4 h + e % 4.  V's operand in that order comes
+// from LDS by transposed reads.
+//
+// DB: blocks of 32 channels; QB: blocks of 32 query rows of a wave.  The four
+// waves share the tiles of K and V: of 64 sources where each has rows of its
+// own, of 128, one block of 32 for each wave, where they share 32 rows (KS).
+// GEN: rows of any width and alignment, staged by elements.
+template <int DB, int QB, bool KS, bool GEN>
+__global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_bf16_kernel(AttnArgs a) {
+    constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;       // 16-byte chunks of a row in LDS
+    constexpr int KT = KS ? 128 : 64;                        // sources of a tile
+    constexpr int NB = KS ? 1 : 2;                           // blocks of 32 of them for a wave
+    constexpr int kTile = KT * CH * 16;                      // bytes of K's or V's tile
+    constexpr int kLoads = KT * CH / kAtThreads;
+    extern __shared__ __align__(16) char lds[];              // [2][K, V]
+
+    const int64_t lb = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (lb >= a.blocks) return;
+    const int split = (int)(lb % a.splits);
+    const int64_t rest = lb / a.splits;
+    const int tile0 = (int)(rest % a.row_tiles);
+    const int64_t pair = rest / a.row_tiles;
+    const int64_t b = pair / a.Hkv;
+    const int kvh = (int)(pair - b * a.Hkv);
+    const int g = a.Hq / a.Hkv;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int half = lane >> 5, col = lane & 31;
+
+    const uint16_t* __restrict__ kp = static_cast<const uint16_t*>(a.k) + b * a.kb + kvh * a.kh;
+    const uint16_t* __restrict__ vp = static_cast<const uint16_t*>(a.v) + b * a.vb + kvh * a.vh;
+    const uint8_t* __restrict__ mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
+    int64_t end = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
+    int64_t begin = 0;
+    if (a.splits > 1) {
+        const int64_t per = ((end + a.splits - 1) / a.splits + KT - 1) / KT * KT;
+        begin = min(end, split * per);
+        end = min(end, begin + per);
+    }
+    const int tiles = (int)((end - begin + KT - 1) / KT);
+
+    // scores are compared and exponentiated in units of 1 / log2(e); a negative scale turns the queries around
+    const float c0 = a.scale * 1.44269504088896340736f;
+    const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
+    const uint32_t qflip = c0 < 0.0f ? 0x80008000u : 0u;
+    const uint32_t qkeep = c0 == 0.0f ? 0u : ~0u;
+
+    // the wave's queries: operand B, channel 16 s + 8 half + e
+    const int row0 = tile0 * (KS ? 32 * QB : 4 * 32 * QB) + (KS ? 0 : wave * 32 * QB);
+    bf16x8 qf[QB][2 * DB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = min(row0 + 32 * qb + col, a.rows - 1);
+        const int n = r / g, h = kvh * g + (r - n * g);
+        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + b * a.qb + n * a.ql + h * a.qh;
+#pragma unroll
+        for (int s = 0; s < 2 * DB; ++s) {
+            const int d0 = 16 * s + 8 * half;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if constexpr (GEN) {
+                uint32_t u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = d0 + e < a.D ? qp[d0 + e] : 0u;
+                w = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+            } else {
+                if (d0 < a.D) w = *reinterpret_cast<const uint4*>(qp + d0);
+            }
+            w.x = (w.x & qkeep) ^ qflip; w.y = (w.y & qkeep) ^ qflip;
+            w.z = (w.z & qkeep) ^ qflip; w.w = (w.w & qkeep) ^ qflip;
+            qf[qb][s] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_cptr)lds;
+    // one tile of K and V to LDS; rows that are not valid, and chunks past D, come as zeros
+    auto stage = [&](int t, const uint64_t (&bits)[KT / 64]) {
+        const int64_t j0 = begin + (int64_t)t * KT;
+        const uint32_t base = lds0 + (t & 1) * 2 * kTile;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int p = i * kAtThreads + tid;
+            const int row = p / CH, ch = (p % CH) ^ at_swz<CH>(row);
+            const bool ok = ((bits[KT == 64 ? 0 : row >> 6] >> (row & 63)) & 1) && 8 * ch < a.D;
+            const int64_t j = j0 + row;
+            if constexpr (GEN) {
+                uint32_t u[8], w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = ok && 8 * ch + e < a.D;
+                    u[e] = in ? kp[j * a.kl + 8 * ch + e] : 0u;
+                    w[e] = in ? vp[j * a.vl + 8 * ch + e] : 0u;
+                }
+                uint4* d = reinterpret_cast<uint4*>(lds + (t & 1) * 2 * kTile) + p;
+                d[0] = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+                d[kTile / 16] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+            } else if (DB != 3 || ch < 4 * DB) {
+                const void* gk = ok ? (const void*)(kp + j * a.kl + 8 * ch) : (const void*)kAtZero;
+                const void* gv = ok ? (const void*)(vp + j * a.vl + 8 * ch) : (const void*)kAtZero;
+                const uint32_t l = __builtin_amdgcn_readfirstlane(base + (i * kAtThreads + wave * 64) * 16);
+                at_load_lds(gk, l);
+                at_load_lds(gv, l + kTile);
+            }
+        }
+    };
+    auto valid_bits = [&](int t, uint64_t (&bits)[KT / 64]) {
+#pragma unroll
+        for (int i = 0; i < KT / 64; ++i) {
+            const int64_t j = begin + (int64_t)t * KT + 64 * i;
+            bits[i] = at_count_bits(j, end);
+            if (mask) bits[i] &= ballot(j + lane < end && mask[j + lane]);
+        }
+    };
+
+    f32x16 oacc[QB][DB];
+    float m[QB], l[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m[qb] = -INFINITY;
+        l[qb] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[qb][d][r] = 0.0f;
+    }
+
+    // a lane's place in the tiles
+    const int swk = at_swz<CH>(col);
+    const int vi = lane & 15, vg = (lane >> 4) & 1;
+    const int vrow = 4 * half + (vi >> 2);                     // + 16 t + 8 (e / 4): bits 0..2 of the source
+    const int vch = 2 * vg + ((vi & 3) >> 1), vin = 8 * (vi & 1);
+
+    uint64_t cur[KT / 64], nxt[KT / 64] = {};
+    if (tiles > 0) {
+        valid_bits(0, cur);
+        stage(0, cur);
+        if (tiles > 1) valid_bits(1, nxt);
+    }
+    for (int t = 0; t < tiles; ++t) {
+        at_wait_loads();
+        __syncthreads();
+        if (t + 1 < tiles) stage(t + 1, nxt);
+        const char* tk = lds + (t & 1) * 2 * kTile;
+        const char* tv = tk + kTile;
+
+        // scores
+        f32x16 s[QB][NB];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int blk = KS ? wave : kb;
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[qb][kb][r] = 0.0f;
+#pragma unroll
+            for (int st = 0; st < 2 * DB; ++st) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tk + (32 * blk + col) * CH * 16 +
+                                                                   (((2 * st + half) ^ swk) << 4));
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    s[qb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][st], s[qb][kb], 0, 0, 0);
+            }
+        }
+        // sources that are not valid
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int blk = KS ? wave : kb;
+            const uint32_t w32 = (uint32_t)(cur[KT == 64 ? 0 : blk >> 1] >> (32 * (blk & 1)));
+            if (w32 != 0xffffffffu) {
+                const uint32_t w = w32 >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool ok = (w >> (8 * (r / 4) + r % 4)) & 1;
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) s[qb][kb][r] = ok ? s[qb][kb][r] : -INFINITY;
+                }
+            }
+        }
+        // weights: the reference m of a query moves when its maximum passes it by 8 (a factor of 256)
+        uint32_t pk[QB][NB][8];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[qb][kb][r]);
+            float lo;
+            const float hi = at_other_half(mx, lo);
+            mx = fmaxf(lo, hi) * c;
+            if (ballot(mx > m[qb] + 8.0f)) {
+                const float mn = fmaxf(m[qb], mx);
+                const float f = mn == -INFINITY ? 1.0f : at_exp2(m[qb] - mn);
+                m[qb] = mn;
+                l[qb] *= f;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) oacc[qb][d][r] *= f;
+            }
+            const float base = m[qb] == -INFINITY ? 0.0f : m[qb];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) {
+                    const float p0 = at_exp2(fmaf(s[qb][kb][r], c, -base));
+                    const float p1 = at_exp2(fmaf(s[qb][kb][r + 1], c, -base));
+                    l[qb] += p0 + p1;
+                    pk[qb][kb][r / 2] = at_pack(p0, p1);
+                }
+        }
+        // outputs
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int blk = KS ? wave : kb;
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    s16x4 v[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = 32 * blk + 16 * st + 8 * e + vrow;
+                        const int ch = (4 * d + vch) ^ (at_swz<CH>(vrow) | e);
+                        v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds_s16x4)(tv + row * CH * 16 + (ch << 4) + vin));
+                    }
+                    const uint4 vw = make_uint4(__builtin_bit_cast(uint2, v[0]).x, __builtin_bit_cast(uint2, v[0]).y,
+                                                __builtin_bit_cast(uint2, v[1]).x, __builtin_bit_cast(uint2, v[1]).y);
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, vw);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) {
+                        const uint4 pw = make_uint4(pk[qb][kb][4 * st], pk[qb][kb][4 * st + 1], pk[qb][kb][4 * st + 2],
+                                                    pk[qb][kb][4 * st + 3]);
+                        oacc[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pw),
+                                                                              oacc[qb][d], 0, 0, 0);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KT / 64; ++i) cur[i] = nxt[i];
+        if (t + 2 < tiles) valid_bits(t + 2, nxt);
+    }
+
+    // the two lanes of a query join their sums
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        float lo;
+        const float hi = at_other_half(l[qb], lo);
+        l[qb] = lo + hi;
+    }
+    constexpr int Dp = 32 * DB;
+    float* pm = a.part ? a.part + (a.blocks / a.row_tiles) * a.rows * Dp : nullptr;
+    if constexpr (KS) {
+        // the waves join: [wave][d][32 rows] sums, then their maxima and sums
+        float* sh = reinterpret_cast<float*>(lds);
+        float* sm = sh + 4 * Dp * 32;
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                sh[(wave * Dp + 32 * d + 8 * (r / 4) + 4 * half + r % 4) * 32 + col] = oacc[0][d][r];
+        if (half == 0) {
+            sm[wave * 32 + col] = m[0];
+            sm[128 + wave * 32 + col] = l[0];
+        }
+        __syncthreads();
+        const int r = tid & 31, row = row0 + r;
+        if (row >= a.rows) return;
+        float mm[4], M = -INFINITY, L = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, mm[w] = sm[w * 32 + r]);
+        const float base = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            mm[w] = at_exp2(mm[w] - base);
+            L += mm[w] * sm[128 + w * 32 + r];
+        }
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        const int n = row / g, h = kvh * g + (row - n * g);
+        uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+        const int64_t pr = (pair * a.splits + split) * a.rows + row;
+        for (int d = tid >> 5; d < a.D; d += kAtThreads / 32) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v += mm[w] * sh[(w * Dp + d) * 32 + r];
+            if (a.splits > 1)
+                a.part[pr * Dp + d] = v;
+            else
+                op[d] = f32_to_bf16_any(v * inv);
+        }
+        if (a.splits > 1 && tid < 32) {
+            pm[2 * pr] = M;
+            pm[2 * pr + 1] = L;
+        }
+    } else {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int row = row0 + 32 * qb + col;
+            if (row >= a.rows) continue;
+            if (a.splits > 1) {
+                const int64_t pr = (pair * a.splits + split) * a.rows + row;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *reinterpret_cast<float4*>(a.part + pr * Dp + 32 * d + 2 * r + 4 * half) = make_float4(
+                            oacc[qb][d][r], oacc[qb][d][r + 1], oacc[qb][d][r + 2], oacc[qb][d][r + 3]);
+                if (half == 0) {
+                    pm[2 * pr] = m[qb];
+                    pm[2 * pr + 1] = l[qb];
+                }
+                continue;
+            }
+            const float inv = l[qb] == 0.0f ? 0.0f : 1.0f / l[qb];
+            const int n = row / g, h = kvh * g + (row - n * g);
+            uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int d0 = 32 * d + 2 * r + 4 * half;
+                    const f32x16 v = oacc[qb][d];
+                    if constexpr (GEN) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (d0 + e < a.D) op[d0 + e] = f32_to_bf16_any(v[r + e] * inv);
+                    } else if (d0 < a.D) {
+                        *reinterpret_cast<uint2*>(op + d0) =
+                            make_uint2(at_pack(v[r] * inv, v[r + 1] * inv), at_pack(v[r + 2] * inv, v[r + 3] * inv));
+                    }
+                }
+        }
+    }
+}
+
+// The splits' results of a row, joined: one wave per row, a channel of four
+// per lane.
+template <typename T>
+__global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, int Dp, int64_t total) {
+    const int64_t e = blockIdx.x * (int64_t)(kAtThreads / 32) + (threadIdx.x >> 5);
+    if (e >= total) return;
+    const int lane = threadIdx.x & 31;
+    const int64_t pair = e / a.rows;
+    const int row = (int)(e - pair * a.rows);
+    const int64_t stride = a.rows, first = pair * a.splits * stride + row;
+    const float* pm = a.part + (total * a.splits) * Dp;
+    float M = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, pm[2 * (first + s * stride)]);
+    const float base = M == -INFINITY ? 0.0f : M;
+    float L = 0.0f, v[4] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const float ms = pm[2 * (first + s * stride)], ls = pm[2 * (first + s * stride) + 1];
+        if (ls == 0.0f) continue;          // no source in this split; its sums may not have been written
+        const float f = at_exp2(ms - base);
+        L += f * ls;
+        if (4 * lane < a.D) {
+            const float4 w = *reinterpret_cast<const float4*>(a.part + (first + s * stride) * Dp + 4 * lane);
+            v[0] += f * w.x; v[1] += f * w.y; v[2] += f * w.z; v[3] += f * w.w;
+        }
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const int g = a.Hq / a.Hkv, n = row / g;
+    const int64_t b = pair / a.Hkv;
+    const int h = (int)(pair - b * a.Hkv) * g + (row - n * g);
+    T* op = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (4 * lane + i >= a.D) break;
+        if constexpr (sizeof(T) == 4)
+            op[4 * lane + i] = v[i] * inv;
+        else
+            op[4 * lane + i] = f32_to_bf16_any(v[i] * inv);
+    }
+}
+
+// How a call is split: QB blocks of query rows per wave, or the waves sharing
+// 32 rows (qb = 0), and `splits` workgroups over the sources.
+struct AttnPlan {
+    int qb, row_tiles, splits, Dp;
+    int64_t blocks;
+};
+
+constexpr int kAtCus = 256;
+
+AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int D) {
+    AttnPlan p;
+    const int64_t pairs = B * Hkv, rows = Nq * (Hq / Hkv);
+    p.Dp = (D + 31) / 32 * 32;
+    p.splits = 1;
+    if (pairs * ceil_div(rows, 256) >= 2 * kAtCus)
+        p.qb = 2;
+    else if (pairs * ceil_div(rows, 128) >= kAtCus)
+        p.qb = 1;
+    else
+        p.qb = 0;
+    p.row_tiles = (int)ceil_div(rows, p.qb ? 128 * p.qb : 32);
+    const int64_t wg = pairs * p.row_tiles;
+    if (p.qb == 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kAtCus / wg, ceil_div(Nk, 256)));
+    p.blocks = wg * p.splits;
+    return p;
+}
+
+size_t attention_ws(const AttnPlan& p, int64_t rows, int64_t pairs) {
+    return p.splits > 1 ? (size_t)(pairs * p.splits * rows * (p.Dp + 2)) * 4 : 0;
+}
+
+template <int DB, int QB, bool KS, bool GEN>
+int launch_attention_bf16(const AttnArgs& a, unsigned grid, hipStream_t s) {
+    constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;
+    constexpr int tiles = 2 * 2 * (KS ? 128 : 64) * CH * 16;
+    constexpr int join = KS ? 4 * 32 * DB * 32 * 4 + 2 * 128 * 4 : 0;
+    constexpr int bytes = tiles > join ? tiles : join;
+    static const hipError_t attr =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_bf16_kernel<DB, QB, KS, GEN>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    MESO_REQUIRE(attr == hipSuccess, MESORASI_EHIP, "mesorasi_cross_attention: LDS size attribute: %s",
+                 hipGetErrorString(attr));
+    attention_bf16_kernel<DB, QB, KS, GEN><<<dim3(grid), dim3(kAtThreads), bytes, s>>>(a);
+    return MESORASI_OK;
+}
+
+template <int DB, bool GEN>
+int launch_attention_bf16(const AttnArgs& a, int qb, unsigned grid, hipStream_t s) {
+    if (qb == 2) return launch_attention_bf16<DB, 2, false, GEN>(a, grid, s);
+    if (qb == 1) return launch_attention_bf16<DB, 1, false, GEN>(a, grid, s);
+    return launch_attention_bf16<DB, 1, true, GEN>(a, grid, s);
+}
+
+template <bool GEN>
+int launch_attention_bf16(const AttnArgs& a, int qb, unsigned grid, hipStream_t s) {
+    switch ((a.D + 31) / 32) {
+        case 1: return launch_attention_bf16<1, GEN>(a, qb, grid, s);
+        case 2: return launch_attention_bf16<2, GEN>(a, qb, grid, s);
+        case 3: return launch_attention_bf16<3, GEN>(a, qb, grid, s);
+        default: return launch_attention_bf16<4, GEN>(a, qb, grid, s);
+    }
+}
+
 }  // namespace
 
 }  // namespace meso
@@ -100,7 +611,11 @@ using namespace meso;
 
 extern "C" size_t mesorasi_cross_attention_workspace(int64_t B, int64_t Nq, int64_t Nk, int32_t Hq, int32_t Hkv,
                                                      int32_t D, int32_t dtype) {
-    return 0;
+    if (B < 1 || Nq < 1 || Nk < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || D < 1 || D > MESORASI_MAX_D_ATTN ||
+        Nk > 0x7fffffff - 1023 || Nq > (0x7fffffff - 1023) / (Hq / Hkv) || B > 0x7fffffff / Hkv)
+        return 0;
+    if (dtype != MESORASI_BF16) return 0;
+    return attention_ws(plan_attention(B, Nq, Nk, Hq, Hkv, D), Nq * (Hq / Hkv), B * Hkv);
 }
 
 extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_ld, int64_t q_hs, const void* k,
@@ -126,13 +641,42 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
                  "mesorasi_cross_attention: Nq = %lld, Nk = %lld", (long long)Nq, (long long)Nk);
     if (B == 0 || Nq == 0) return MESORASI_OK;
     MESO_REQUIRE(q && o && (Nk == 0 || (k && v)), MESORASI_EINVAL, "mesorasi_cross_attention: NULL q, k, v or o");
+    MESO_REQUIRE(B <= 0x7fffffff / Hkv, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: B = %lld", (long long)B);
     AttnArgs a = {q, k, v, o, q_bs, q_ld, q_hs, k_bs, k_ld, k_hs, v_bs, v_ld, v_hs, o_bs, o_ld, o_hs,
                   Nq, Nk, mask_ld, Hq, Hkv, D, scale, k_len, k_mask};
-    const int64_t total = B * Nq * Hq;
-    MESO_REQUIRE(total <= 0x7fffffff, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: size");
-    if (dtype == MESORASI_F32)
-        attention_kernel<float><<<dim3((unsigned)total), dim3(64), 0, as_stream(stream)>>>(a, total);
-    else
-        attention_kernel<uint16_t><<<dim3((unsigned)total), dim3(64), 0, as_stream(stream)>>>(a, total);
+    hipStream_t s = as_stream(stream);
+    if (dtype == MESORASI_F32) {
+        const int64_t total = B * Nq * Hq;
+        MESO_REQUIRE(total <= 0x7fffffff, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: size");
+        attention_kernel<float><<<dim3((unsigned)total), dim3(64), 0, s>>>(a, total);
+        return after_launch("mesorasi_cross_attention");
+    }
+    const AttnPlan p = plan_attention(B, Nq, Nk, Hq, Hkv, D);
+    const int64_t pairs = B * Hkv;
+    a.rows = (int)(Nq * (Hq / Hkv));
+    const size_t need = attention_ws(p, a.rows, pairs);
+    MESO_REQUIRE(need == 0 || (ws && ws_bytes >= need), MESORASI_EWORKSPACE,
+                 "mesorasi_cross_attention: workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+    MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_cross_attention: ws is not 16-byte aligned");
+    a.row_tiles = p.row_tiles;
+    a.splits = p.splits;
+    a.blocks = p.blocks;
+    a.part = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
+    const int64_t per = ceil_div(p.blocks, 8);
+    MESO_REQUIRE(per <= 0x7fffffff / 8, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
+                 (long long)p.blocks);
+    a.per_xcd = (int)per;
+    // 16-byte chunks of every row, 8-byte pieces of the output
+    const int64_t st = q_bs | q_ld | q_hs | k_bs | k_ld | k_hs | v_bs | v_ld | v_hs | D;
+    const bool vec = st % 8 == 0 && (o_bs | o_ld | o_hs) % 4 == 0 && aligned(q, 16) && aligned(k, 16) &&
+                     aligned(v, 16) && aligned(o, 8);
+    const int rc = vec ? launch_attention_bf16<false>(a, p.qb, (unsigned)(8 * per), s)
+                       : launch_attention_bf16<true>(a, p.qb, (unsigned)(8 * per), s);
+    if (rc != MESORASI_OK) return rc;
+    if (p.splits > 1) {
+        const int64_t total = pairs * a.rows;
+        attention_join_kernel<uint16_t>
+            <<<dim3((unsigned)ceil_div(total, kAtThreads / 32)), dim3(kAtThreads), 0, s>>>(a, p.Dp, total);
+    }
     return after_launch("mesorasi_cross_attention");
 }
