@@ -117,16 +117,16 @@ __device__ const uint4 kAtZero[1] = {};
 
 // Slot of a 16-byte chunk in its row of CH chunks: rows that one read
 // touches together lie in different banks (the scores read one chunk of 16
-// rows, the transposed reads two chunks of 8 rows).
+// rows, half of a transposed read four chunks of 4 rows).
 template <int CH>
 __device__ __forceinline__ int at_swz(int row) {
-    const int top = (row >> 3) & 1;
+    const int low = (row >> 2) & 3;
     if constexpr (CH == 16)
-        return ((row & 7) << 1) | top;
+        return ((row & 3) << 2) | low;
     else if constexpr (CH == 8)
-        return (((row >> 1) & 3) << 1) | top;
+        return (((row >> 1) & 1) << 2) | low;
     else
-        return (((row >> 2) & 1) << 1) | top;
+        return low;
 }
 
 // 16 bytes from each lane's address to LDS at base + 16 lane.  The wait is
@@ -172,7 +172,7 @@ __device__ __forceinline__ uint64_t at_count_bits(int64_t j0, int64_t end) {
 // own, of 128, one block of 32 for each wave, where they share 32 rows (KS).
 // GEN: rows of any width and alignment, staged by elements.
 template <int DB, int QB, bool KS, bool GEN>
-__global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_bf16_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs a) {
     constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;       // 16-byte chunks of a row in LDS
     constexpr int KT = KS ? 128 : 64;                        // sources of a tile
     constexpr int NB = KS ? 1 : 2;                           // blocks of 32 of them for a wave
@@ -288,6 +288,7 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
             for (int r = 0; r < 16; ++r) oacc[qb][d][r] = 0.0f;
     }
 
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
     // a lane's place in the tiles
     const int swk = at_swz<CH>(col);
     const int vi = lane & 15, vg = (lane >> 4) & 1;
@@ -307,24 +308,31 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
         const char* tk = lds + (t & 1) * 2 * kTile;
         const char* tv = tk + kTile;
 
-        // scores
+        // scores: the next block's operands are read between this block's products
         f32x16 s[QB][NB];
+        bf16x8 kf[2][2 * DB];
+        auto read_k = [&](int kb, int st) {
+            const int blk = KS ? wave : kb;
+            return *reinterpret_cast<const bf16x8*>(tk + (32 * blk + col) * CH * 16 + (((2 * st + half) ^ swk) << 4));
+        };
+#pragma unroll
+        for (int st = 0; st < 2 * DB; ++st) kf[0][st] = read_k(0, st);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
-            const int blk = KS ? wave : kb;
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[qb][kb][r] = 0.0f;
 #pragma unroll
             for (int st = 0; st < 2 * DB; ++st) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tk + (32 * blk + col) * CH * 16 +
-                                                                   (((2 * st + half) ^ swk) << 4));
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
-                    s[qb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][st], s[qb][kb], 0, 0, 0);
+                    s[qb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kb & 1][st], qf[qb][st], s[qb][kb], 0, 0, 0);
+                if (kb + 1 < NB) kf[(kb + 1) & 1][st] = read_k(kb + 1, st);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         // sources that are not valid
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
@@ -367,10 +375,12 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
             for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int r = 0; r < 16; r += 2) {
+                    // the sum takes the rounded weights, as the product with V does
                     const float p0 = at_exp2(fmaf(s[qb][kb][r], c, -base));
                     const float p1 = at_exp2(fmaf(s[qb][kb][r + 1], c, -base));
-                    l[qb] += p0 + p1;
                     pk[qb][kb][r / 2] = at_pack(p0, p1);
+                    l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[qb][kb][r / 2]), ones, l[qb],
+                                                            false);
                 }
         }
         // outputs
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int row = 32 * blk + 16 * st + 8 * e + vrow;
-                        const int ch = (4 * d + vch) ^ (at_swz<CH>(vrow) | e);
+                        const int ch = (4 * d + vch) ^ (at_swz<CH>(vrow) | 2 * e);
                         v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                             (lds_s16x4)(tv + row * CH * 16 + (ch << 4) + vin));
                     }
@@ -414,9 +424,8 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
         const float hi = at_other_half(l[qb], lo);
         l[qb] = lo + hi;
     }
-    constexpr int Dp = 32 * DB;
-    float* pm = a.part ? a.part + (a.blocks / a.row_tiles) * a.rows * Dp : nullptr;
     if constexpr (KS) {
+        constexpr int Dp = 32 * DB;
         // the waves join: [wave][d][32 rows] sums, then their maxima and sums
         float* sh = reinterpret_cast<float*>(lds);
         float* sm = sh + 4 * Dp * 32;
@@ -456,6 +465,7 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
                 op[d] = f32_to_bf16_any(v * inv);
         }
         if (a.splits > 1 && tid < 32) {
+            float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * Dp;
             pm[2 * pr] = M;
             pm[2 * pr + 1] = L;
         }
@@ -464,20 +474,6 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
         for (int qb = 0; qb < QB; ++qb) {
             const int row = row0 + 32 * qb + col;
             if (row >= a.rows) continue;
-            if (a.splits > 1) {
-                const int64_t pr = (pair * a.splits + split) * a.rows + row;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4)
-                        *reinterpret_cast<float4*>(a.part + pr * Dp + 32 * d + 2 * r + 4 * half) = make_float4(
-                            oacc[qb][d][r], oacc[qb][d][r + 1], oacc[qb][d][r + 2], oacc[qb][d][r + 3]);
-                if (half == 0) {
-                    pm[2 * pr] = m[qb];
-                    pm[2 * pr + 1] = l[qb];
-                }
-                continue;
-            }
             const float inv = l[qb] == 0.0f ? 0.0f : 1.0f / l[qb];
             const int n = row / g, h = kvh * g + (row - n * g);
             uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
@@ -500,44 +496,63 @@ __global__ __launch_bounds__(kAtThreads, (DB * QB > 4 ? 1 : 2)) void attention_b
     }
 }
 
-// The splits' results of a row, joined: one wave per row, a channel of four
-// per lane.
+constexpr int kAtMaxSplits = 256;
+
+// The splits' results of one row, joined: their weights first, a split per
+// thread, then the sums, 32 lanes of 4 channels over every eighth split.
 template <typename T>
-__global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, int Dp, int64_t total) {
-    const int64_t e = blockIdx.x * (int64_t)(kAtThreads / 32) + (threadIdx.x >> 5);
-    if (e >= total) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t pair = e / a.rows;
-    const int row = (int)(e - pair * a.rows);
-    const int64_t stride = a.rows, first = pair * a.splits * stride + row;
-    const float* pm = a.part + (total * a.splits) * Dp;
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, pm[2 * (first + s * stride)]);
-    const float base = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, v[4] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float ms = pm[2 * (first + s * stride)], ls = pm[2 * (first + s * stride) + 1];
-        if (ls == 0.0f) continue;          // no source in this split; its sums may not have been written
-        const float f = at_exp2(ms - base);
-        L += f * ls;
-        if (4 * lane < a.D) {
-            const float4 w = *reinterpret_cast<const float4*>(a.part + (first + s * stride) * Dp + 4 * lane);
-            v[0] += f * w.x; v[1] += f * w.y; v[2] += f * w.z; v[3] += f * w.w;
+__global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, int Dp) {
+    __shared__ float w[kAtMaxSplits], red[4];
+    __shared__ float4 sum[kAtThreads / 32][32];
+    const int tid = threadIdx.x, lane = tid & 31, grp = tid >> 5;
+    const int64_t pair = blockIdx.x / a.rows;
+    const int row = (int)(blockIdx.x - pair * a.rows);
+    const int64_t first = pair * a.splits * a.rows + row;
+    const float* pm = a.part + (int64_t)gridDim.x * a.splits * Dp;
+    float m = -INFINITY, l = 0.0f;
+    if (tid < a.splits) {
+        const float2 v = *reinterpret_cast<const float2*>(pm + 2 * (first + tid * (int64_t)a.rows));
+        m = v.x;
+        l = v.y;
+    }
+    float M = wave_max_f32(m);
+    if ((tid & 63) == 0) red[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    // a split without any source has l = 0; its sums may not have been written
+    const float f = l == 0.0f ? 0.0f : at_exp2(m - (M == -INFINITY ? 0.0f : M));
+    w[tid] = f;
+    float L = f * l;
+    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
+    __syncthreads();
+    if ((tid & 63) == 0) red[tid >> 6] = L;
+    __syncthreads();
+    L = (red[0] + red[1]) + (red[2] + red[3]);
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (4 * lane < a.D) {
+#pragma unroll 4
+        for (int s = grp; s < a.splits; s += kAtThreads / 32) {
+            const float fs = w[s];
+            if (fs == 0.0f) continue;
+            const float4 x = *reinterpret_cast<const float4*>(a.part + (first + s * (int64_t)a.rows) * Dp + 4 * lane);
+            v.x += fs * x.x; v.y += fs * x.y; v.z += fs * x.z; v.w += fs * x.w;
         }
     }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    sum[grp][lane] = v;
+    __syncthreads();
+    if (tid >= a.D) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAtThreads / 32; ++i) t += reinterpret_cast<const float*>(sum[i])[tid];
+    t *= L == 0.0f ? 0.0f : 1.0f / L;
     const int g = a.Hq / a.Hkv, n = row / g;
     const int64_t b = pair / a.Hkv;
     const int h = (int)(pair - b * a.Hkv) * g + (row - n * g);
     T* op = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (4 * lane + i >= a.D) break;
-        if constexpr (sizeof(T) == 4)
-            op[4 * lane + i] = v[i] * inv;
-        else
-            op[4 * lane + i] = f32_to_bf16_any(v[i] * inv);
-    }
+    if constexpr (sizeof(T) == 4)
+        op[tid] = t;
+    else
+        op[tid] = f32_to_bf16_any(t);
 }
 
 // How a call is split: QB blocks of query rows per wave, or the waves sharing
@@ -554,15 +569,15 @@ AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int 
     const int64_t pairs = B * Hkv, rows = Nq * (Hq / Hkv);
     p.Dp = (D + 31) / 32 * 32;
     p.splits = 1;
-    if (pairs * ceil_div(rows, 256) >= 2 * kAtCus)
+    if (D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
         p.qb = 2;
-    else if (pairs * ceil_div(rows, 128) >= kAtCus)
+    else if (pairs * ceil_div(rows, 128) >= kAtCus * 3 / 4)
         p.qb = 1;
     else
         p.qb = 0;
     p.row_tiles = (int)ceil_div(rows, p.qb ? 128 * p.qb : 32);
     const int64_t wg = pairs * p.row_tiles;
-    if (p.qb == 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kAtCus / wg, ceil_div(Nk, 256)));
+    if (p.qb == 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 256)));
     p.blocks = wg * p.splits;
     return p;
 }
@@ -588,7 +603,8 @@ int launch_attention_bf16(const AttnArgs& a, unsigned grid, hipStream_t s) {
 
 template <int DB, bool GEN>
 int launch_attention_bf16(const AttnArgs& a, int qb, unsigned grid, hipStream_t s) {
-    if (qb == 2) return launch_attention_bf16<DB, 2, false, GEN>(a, grid, s);
+    if constexpr (DB <= 2)
+        if (qb == 2) return launch_attention_bf16<DB, 2, false, GEN>(a, grid, s);
     if (qb == 1) return launch_attention_bf16<DB, 1, false, GEN>(a, grid, s);
     return launch_attention_bf16<DB, 1, true, GEN>(a, grid, s);
 }
@@ -674,9 +690,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
                        : launch_attention_bf16<true>(a, p.qb, (unsigned)(8 * per), s);
     if (rc != MESORASI_OK) return rc;
     if (p.splits > 1) {
-        const int64_t total = pairs * a.rows;
-        attention_join_kernel<uint16_t>
-            <<<dim3((unsigned)ceil_div(total, kAtThreads / 32)), dim3(kAtThreads), 0, s>>>(a, p.Dp, total);
+        attention_join_kernel<uint16_t><<<dim3((unsigned)(pairs * a.rows)), dim3(kAtThreads), 0, s>>>(a, p.Dp);
     }
     return after_launch("mesorasi_cross_attention");
 }

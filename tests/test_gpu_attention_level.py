@@ -402,6 +402,36 @@ def test_attention(gpu, dtype, B, Nq, Nk, Hq, Hkv, D):
            *_ref_and_bound(q, k, v, k_len=k_len, k_mask=mask, scale=0.3), "both")
 
 
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("B,Nq,Nk,Hq,Hkv,D", [
+    (64, 300, 70, 8, 8, 64), (64, 270, 131, 8, 8, 24), (32, 300, 65, 16, 8, 30), (64, 257, 5, 8, 8, 61),
+    (16, 200, 150, 8, 4, 128), (16, 200, 64, 8, 4, 88), (16, 190, 100, 8, 4, 119), (24, 130, 193, 8, 4, 64),
+    (16, 260, 70, 4, 4, 69),
+])
+def test_attention_many_workgroups(gpu, dtype, B, Nq, Nk, Hq, Hkv, D):
+    """Enough rows for the forms that give every wave rows of its own."""
+    g = gen(Nq + Nk + D)
+    q, k, v = (randn(g, B, n, h, D, dtype=dtype) for n, h in ((Nq, Hq), (Nk, Hkv), (Nk, Hkv)))
+    within(ops.cross_attention(q, k, v), *_ref_and_bound(q, k, v))
+    k_len = torch.tensor([(Nk * (b % 9)) // 8 for b in range(B)], dtype=torch.int32, device="cuda")
+    mask = torch.rand((B, Nk), generator=g, device="cuda") < 0.7
+    kw = dict(k_len=k_len, k_mask=mask, scale=-0.2)
+    ref, bound = _ref_and_bound(q, k, v, **kw)
+    ok = mask & (torch.arange(Nk, device="cuda")[None] < k_len[:, None])
+    k, v = (torch.where(ok[:, :, None, None], t, torch.full((), math.nan, dtype=dtype, device="cuda")) for t in (k, v))
+    within(ops.cross_attention(q, k, v, **kw), ref, bound, "counts and mask")
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+def test_attention_scale_zero(gpu, dtype):
+    """A scale of 0 gives the mean of the valid sources."""
+    g = gen(21)
+    q, k, v = (randn(g, 2, n, 2, 16, dtype=dtype) for n in (3, 50, 50))
+    k_len = torch.tensor([50, 20], dtype=torch.int32, device="cuda")
+    o, bound = _ref_and_bound(q, k, v, k_len=k_len, scale=0.0)
+    within(ops.cross_attention(q, k, v, k_len=k_len, scale=0.0), o, bound)
+
+
 def _ref_and_bound(q, k, v, **kw):
     o, size, top = attention_ref(q, k, v, **kw)
     return o, attention_bound(o, size, top, q.shape[-1], q.dtype)
