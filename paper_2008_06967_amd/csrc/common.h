@@ -117,6 +117,59 @@ __device__ __forceinline__ int wave_max_i32(int v) {
     return __builtin_amdgcn_readlane(v, 63);
 }
 
+// Division of 0 <= n < 2^31 by a fixed d >= 1: with l = ceil(log2 d) and M =
+// ceil(2^(32 + l) / d), n / d is n M / 2^(32 + l) rounded down; M - 2^32 is kept.
+struct FastDiv {
+    uint32_t d, m, l;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t div) : d(div), m(0), l(0) {
+        while ((1ull << l) < div) ++l;
+        m = (uint32_t)((((1ull << l) - div) << 32) / div + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> l); }
+    __device__ __forceinline__ int div(int n, int& rem) const {
+        const int q = div(n);
+        rem = n - q * (int)d;
+        return q;
+    }
+};
+
+// Sum over the lanes that differ from a lane in the bits from log2(from) up
+// (from a power of two, 1 to 64): rotations of the 16-lane rows, then swaps of
+// rows and halves.  Lanes may add in different orders.
+__device__ __forceinline__ float wave_sum_from(float v, int from) {
+    if (from <= 1) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x121, 0xf, 0xf, true));
+    if (from <= 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x122, 0xf, 0xf, true));
+    if (from <= 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xf, 0xf, true));
+    if (from <= 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xf, 0xf, true));
+    if (from <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (from <= 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
+// Sum over groups of w lanes (a power of two, 1 to 64).
+__device__ __forceinline__ float lane_sum(float v, int w) {
+    if (w > 1) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));    // lane ^ 1
+    if (w > 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));    // lane ^ 2
+    if (w > 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));   // 7 - lane
+    if (w > 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, true));   // 15 - lane
+    if (w > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (w > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
 // Compute units of the current device.
 inline int device_cus() {
     int dev = 0, cus = 256;

@@ -1,4 +1,19 @@
 // Group normalisation with an activation, channels last.
+//
+// Mean and variance are joined from parts, each (count, mean, sum of squared
+// differences to that mean), so that nothing cancels: a thread sums
+// differences to its own first value, parts join by differences of their
+// means, and means are kept relative to the group's first value, so that an
+// offset of the data costs no accuracy.  Parts are joined in a fixed order.
+//
+// Two forms.  Where the rows of a run of whole groups fit the registers of
+// one workgroup, it reads them once, and one launch does all.  Otherwise one
+// launch forms the parts of chunks of rows and another joins them and
+// writes; its writes pass the caches by, which leaves them to x: 141 us
+// instead of 178 for 16 x 16384 x 256 in fp32.
+//
+// Bound: one read and one write of HBM, and a second read where x is larger
+// than the caches.
 #include <algorithm>
 #include <cmath>
 
@@ -8,77 +23,559 @@ namespace meso {
 
 namespace {
 
-constexpr int kGnThreads = 256;
+constexpr int kGnThreads = 256;      // of the two-launch form
+constexpr int kGnOneThreads = 512;   // of the one-launch form
+constexpr int kGnKeep = 16;          // vectors of a thread in the one-launch form
+constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) GnVec {
+    T e[N];
+};
+
+struct GnArgs {
+    const void* x;
+    void* y;
+    const int32_t* lens;
+    const float* gamma;
+    const float* beta;
+    float2* part;                    // [B, chunks, groups, pieces]: mean, sum of squared differences
+    int64_t ldx, ldy, B, N;
+    int C, G, c;
+    float eps;
+    int act;
+    int slab;                        // channels of a workgroup: whole groups, or a piece of one
+    int slabs, pieces;               // slabs of a row; slabs of a group (1: whole groups in a slab)
+    int chunks;
+    int64_t chunk_rows;
+    FastDiv by_chunks, by_slabs, by_pieces, by_c;
+    FastDiv by_rows;                 // rows of a chunk
+    FastDiv by_nv;                   // vectors of a full slab
+};
+
+__device__ __forceinline__ float gn_float(float v) { return v; }
+__device__ __forceinline__ float gn_float(uint16_t v) { return bf16_to_f32(v); }
 
 template <typename T>
-__device__ __forceinline__ float gn_load(const T* p) {
+__device__ __forceinline__ T gn_round(float v) {
     if constexpr (sizeof(T) == 4)
-        return *p;
+        return v;
     else
-        return bf16_to_f32(*p);
+        return f32_to_bf16_any(v);
 }
 
-template <typename T>
-__device__ __forceinline__ void gn_store(T* p, float v) {
-    if constexpr (sizeof(T) == 4)
-        *p = v;
-    else
-        *p = f32_to_bf16_any(v);
+// erfc(z), z >= 0, as 2 to a polynomial: a least-maximum fit of log2(erfc) on
+// [0, 4] weighted for z erfc(z) (within 5e-8 in fp32); past 4 it falls faster
+// than log2(erfc), where z erfc(z) is below 7e-8.
+__device__ __forceinline__ float gn_erfc(float z) {
+    float p = -1.7592439007785288e-06f;
+    p = fmaf(p, z, 3.0905426683602855e-05f);
+    p = fmaf(p, z, -0.00024038320407271385f);
+    p = fmaf(p, z, 0.0010606396244838834f);
+    p = fmaf(p, z, -0.002575934398919344f);
+    p = fmaf(p, z, 0.00033866698504425585f);
+    p = fmaf(p, z, 0.02760038711130619f);
+    p = fmaf(p, z, -0.14827527105808258f);
+    p = fmaf(p, z, -0.9184468388557434f);
+    p = fmaf(p, z, -1.627907156944275f);
+    return __builtin_amdgcn_exp2f(p * z);
 }
 
-__device__ __forceinline__ float gn_act(float v, int act) {
-    switch (act) {
-        case MESORASI_ACT_RELU: return v < 0.0f ? 0.0f : v;
-        case MESORASI_ACT_SILU: return v / (1.0f + expf(-v));
-        case MESORASI_ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678f));
-        default: return v;
+// A store that passes the caches by.
+template <typename T, int N>
+__device__ __forceinline__ void gn_store(T* p, const GnVec<T, N>& v) {
+    if constexpr (sizeof(T) * N >= 4) {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * N >= 16 ? 4 : sizeof(T) * N / 4)));
+        const words* w = reinterpret_cast<const words*>(&v);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) * N / sizeof(words)); ++i)
+            __builtin_nontemporal_store(w[i], reinterpret_cast<words*>(p) + i);
+    } else {
+        __builtin_nontemporal_store(v.e[0], p);
     }
 }
 
-__device__ __forceinline__ float gn_block_sum(float v, float* sh) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float t = 0.0f;
-    for (int i = 0; i < kGnThreads / 64; ++i) t += sh[i];
-    return t;
+template <int ACT>
+__device__ __forceinline__ float gn_act(float v) {
+    if constexpr (ACT == MESORASI_ACT_RELU) return v < 0.0f ? 0.0f : v;
+    if constexpr (ACT == MESORASI_ACT_SILU)
+        return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
+    if constexpr (ACT == MESORASI_ACT_GELU) {
+        const float e = gn_erfc(fabsf(v) * 0.70710678f);
+        return 0.5f * v * (v < 0.0f ? e : 2.0f - e);
+    }
+    return v;
 }
 
-// One workgroup per cloud and group: mean, variance, output, a pass each.
-template <typename TX, typename TY>
-__global__ __launch_bounds__(kGnThreads) void group_norm_kernel(const TX* __restrict__ x, int64_t ldx, int64_t N, int C,
-                                                                int G, const int32_t* __restrict__ lens,
-                                                                const float* __restrict__ gamma,
-                                                                const float* __restrict__ beta, float eps, int act,
-                                                                TY* __restrict__ y, int64_t ldy) {
-    __shared__ float sh[kGnThreads / 64];
-    const int64_t b = blockIdx.x / G;
-    const int g = (int)(blockIdx.x % G), c = C / G;
-    const int64_t n = lens ? min(max((int64_t)lens[b], (int64_t)0), N) : N;
-    const TX* xb = x + b * N * ldx + (int64_t)g * c;
-    TY* yb = y + b * N * ldy + (int64_t)g * c;
-    const int64_t total = n * c;
-    // differences to a value of the group keep the spread's precision
-    const float pv = n > 0 ? gn_load(xb) : 0.0f;
-    float s = 0.0f;
-    for (int64_t i = threadIdx.x; i < total; i += kGnThreads) s += gn_load(xb + (i / c) * ldx + i % c) - pv;
-    const float mu = gn_block_sum(s, sh) / (float)total;
-    s = 0.0f;
-    for (int64_t i = threadIdx.x; i < total; i += kGnThreads) {
-        const float d = gn_load(xb + (i / c) * ldx + i % c) - pv - mu;
-        s += d * d;
+// Lanes that share a group's parts: all threads at work at once, at most a wave for a group.
+template <int THREADS>
+__device__ __forceinline__ int gn_lanes(int groups, int parts) {
+    int w = 1;
+    while (w < 64 && w < parts && 2 * w * groups <= THREADS) w *= 2;
+    return __builtin_amdgcn_readfirstlane(w);
+}
+
+// The groups' parts in LDS, joined: part (s, e), e < per, of a group counts
+// n(s) values and is get(g, s, e) = (mean, sum of squares); put(g, n, mean,
+// m2) takes the result.
+template <int THREADS, typename Count, typename Get, typename Put>
+__device__ __forceinline__ void gn_join(int groups, int slots, int per, Count n, Get get, Put put) {
+    const int w = gn_lanes<THREADS>(groups, slots * per);
+    int we = 1;
+    while (we < w && we < per) we *= 2;
+    const int lw = __builtin_ctz(w), le = __builtin_ctz(we);
+    const int lane = threadIdx.x & (w - 1), ws = w >> le, s0 = lane >> le, e0 = lane & (we - 1);
+    for (int g = threadIdx.x >> lw; g < groups; g += THREADS >> lw) {
+        const float m0 = get(g, 0, 0).x;
+        float cnt = 0.0f, sum = 0.0f;
+        for (int s = s0; s < slots; s += ws)
+            for (int e = e0; e < per; e += we) {
+                const float k = n(s);
+                cnt += k;
+                sum += k * (get(g, s, e).x - m0);
+            }
+        cnt = lane_sum(cnt, w);
+        const float d = lane_sum(sum, w) / cnt;
+        float m2 = 0.0f;
+        for (int s = s0; s < slots; s += ws)
+            for (int e = e0; e < per; e += we) {
+                const float2 v = get(g, s, e);
+                const float t = (v.x - m0) - d;
+                m2 += v.y + n(s) * t * t;
+            }
+        m2 = lane_sum(m2, w);
+        if (lane == 0) put(g, cnt, m0 + d, m2);
     }
-    const float rs = 1.0f / sqrtf(gn_block_sum(s, sh) / (float)total + eps);
-    for (int64_t i = threadIdx.x; i < N * c; i += kGnThreads) {
-        const int64_t r = i / c;
-        const int ch = (int)(i % c), cc = g * c + ch;
-        float v = 0.0f;
-        if (r < n) {
-            v = (gn_load(xb + r * ldx + ch) - pv - mu) * rs;
-            v = gn_act(v * (gamma ? gamma[cc] : 1.0f) + (beta ? beta[cc] : 0.0f), act);
+}
+
+// A workgroup's place: cloud, slab, valid rows, and each thread's vector of
+// channels and rows.
+template <int THREADS, int VEC>
+struct GnPlace {
+    int64_t b, len;
+    int slab, ch0, width, slots, slot, vec, first, groups;
+    bool on;
+    __device__ GnPlace(const GnArgs& a, int blk) {     // cloud and slab
+        b = a.by_slabs.div(blk, slab);
+        len = a.lens ? min(max((int64_t)a.lens[b], (int64_t)0), a.N) : a.N;
+        if (a.pieces > 1) {
+            int piece;
+            first = a.by_pieces.div(slab, piece);
+            ch0 = first * a.c + piece * a.slab;
+            width = min(a.slab, a.c - piece * a.slab);
+            groups = 1;
+        } else {
+            ch0 = slab * a.slab;
+            width = min(a.slab, a.C - ch0);
+            first = a.by_c.div(ch0);
+            groups = a.by_c.div(width);
         }
-        gn_store(yb + r * ldy + ch, v);
+        // a narrower slab leaves lanes of a row without work
+        slots = THREADS / (int)a.by_nv.d;
+        slot = a.by_nv.div(threadIdx.x, vec);
+        on = slot < slots && vec * VEC < width;
+    }
+    // the groups, within the slab, of the thread's channels
+    __device__ void channel_groups(const GnArgs& a, int (&g)[VEC]) const {
+        int n = 0, r = 0;
+        if (on && a.pieces == 1) {
+            n = a.by_c.div(vec * VEC, r);
+        }
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            g[k] = n;
+            if (++r == a.c && a.pieces == 1) {
+                ++n;
+                r = 0;
+            }
+        }
+    }
+};
+
+// A thread's channels: their groups, each group's first value (what its rows
+// are compared with), gamma and beta.
+template <int VEC>
+struct GnChannels {
+    int grp[VEC];
+    float ref[VEC], gamma[VEC], beta[VEC];
+};
+
+template <typename TX, int VEC, bool AFFINE, typename P>
+__device__ __forceinline__ void gn_channels(const GnArgs& a, const P& p, GnChannels<VEC>& c) {
+    const TX* x0 = static_cast<const TX*>(a.x) + p.b * a.N * a.ldx + (int64_t)p.first * a.c;
+    p.channel_groups(a, c.grp);
+    const int ch = p.ch0 + p.vec * VEC;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        c.ref[k] = p.on && p.len > 0 ? gn_float(x0[c.grp[k] * a.c]) : 0.0f;
+        if (AFFINE) {
+            c.gamma[k] = p.on && a.gamma ? a.gamma[ch + k] : 1.0f;
+            c.beta[k] = p.on && a.beta ? a.beta[ch + k] : 0.0f;
+        }
+    }
+}
+
+// The thread's channels' parts (mean relative to its group's first value,
+// squares) to LDS: channels of one group join at once.
+template <int VEC>
+__device__ __forceinline__ void gn_put_parts(bool merged, float n, const float (&mean)[VEC], const float (&m2)[VEC],
+                                             float2* ent) {
+    if (!merged) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) ent[k] = make_float2(mean[k], m2[k]);
+        return;
+    }
+    float d = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int k = 1; k < VEC; ++k) d += mean[k] - mean[0];
+    d *= 1.0f / VEC;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        const float t = (mean[k] - mean[0]) - d;
+        q += m2[k] + n * t * t;
+    }
+    *ent = make_float2(mean[0] + d, q);
+}
+
+template <typename TX, int VEC>
+__global__ __launch_bounds__(kGnThreads) void gn_parts_kernel(GnArgs a) {
+    __shared__ float2 ent[kGnThreads * VEC];
+    int chunk;
+    const int rest = a.by_chunks.div((int)blockIdx.x, chunk);
+    const GnPlace<kGnThreads, VEC> p(a, rest);
+    const int64_t r0 = chunk * a.chunk_rows, r1 = min(p.len, r0 + a.chunk_rows);
+    if (r0 >= r1) return;                        // no valid row: the join knows
+    const int nrows = (int)(r1 - r0);
+    const bool merged = a.pieces > 1 || a.c % VEC == 0;
+    GnChannels<VEC> c;
+    gn_channels<TX, VEC, false>(a, p, c);
+    float sum[VEC] = {}, sq[VEC] = {}, f[VEC] = {};
+    const int full = nrows / p.slots, tail = nrows - full * p.slots;      // rows of every slot, slots with one more
+    const int mine = p.on ? full + (p.slot < tail) : 0;
+    if (mine > 0) {
+        const TX* xp = static_cast<const TX*>(a.x) + (p.b * a.N + r0 + p.slot) * a.ldx + p.ch0 + p.vec * VEC;
+        const int64_t step = (int64_t)p.slots * a.ldx;
+        GnVec<TX, VEC> w = *reinterpret_cast<const GnVec<TX, VEC>*>(xp);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] = gn_float(w.e[k]);
+#pragma unroll 4
+        for (int i = 1; i < mine; ++i) {
+            w = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + i * step);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const float d = gn_float(w.e[k]) - f[k];
+                sum[k] += d;
+                sq[k] = fmaf(d, d, sq[k]);
+            }
+        }
+        const float n = (float)mine;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float d = sum[k] / n;
+            sq[k] -= sum[k] * d;
+            f[k] = (f[k] - c.ref[k]) + d;
+        }
+    }
+    const int nv = (int)a.by_nv.d;
+    if (p.on) gn_put_parts<VEC>(merged, (float)mine, f, sq, ent + (p.slot * nv + p.vec) * (merged ? 1 : VEC));
+    __syncthreads();
+    const int per_slot = merged ? nv : nv * VEC;             // parts of a slot
+    const int per = merged ? (a.pieces > 1 ? p.width : a.c) / VEC : a.c;   // of them, a group's
+    const float each = merged ? (float)VEC : 1.0f;
+    const int groups_all = a.G * a.pieces;
+    float2* out = a.part + (p.b * a.chunks + chunk) * groups_all +
+                  (a.pieces > 1 ? p.slab : p.first);
+    gn_join<kGnThreads>(
+        p.groups, min(p.slots, nrows), per,
+        [&](int s) { return (float)(s < tail ? full + 1 : full) * each; },
+        [&](int g, int s, int e) { return ent[s * per_slot + g * per + e]; },
+        [&](int g, float, float mean, float m2) { out[g] = make_float2(mean, m2); });
+}
+
+// y = act((x - ref) A + S): A = gamma / sqrt(var + eps), S = beta - (mean -
+// ref) A, from st = (mean - ref, 1 / sqrt(var + eps)).
+__device__ __forceinline__ void gn_factor(float2 st, float gamma, float beta, float& A, float& S) {
+    A = st.y * gamma;
+    S = fmaf(-st.x, A, beta);
+}
+
+// The cloud's parts in memory, joined: (mean, 1 / deviation) of the slab's
+// groups.  The first kGnBatch parts of a lane are all on their way at once.
+constexpr int kGnBatch = 8;
+
+template <typename P>
+__device__ __forceinline__ void gn_join_chunks(const GnArgs& a, const P& p, float2* stat) {
+    const int groups_all = a.G * a.pieces;
+    const int used = a.by_rows.div((int)p.len - 1) + 1, total = used * a.pieces;
+    const int w = gn_lanes<kGnThreads>(p.groups, total);
+    const int lane = threadIdx.x & (w - 1), lw = __builtin_ctz(w);
+    for (int g = threadIdx.x >> lw; g < p.groups; g += kGnThreads >> lw) {
+        const float2* in = a.part + p.b * a.chunks * groups_all + (p.first + g) * a.pieces;
+        auto get = [&](int i) {
+            const int chunk = a.pieces > 1 ? a.by_pieces.div(i) : i;
+            return in[(int64_t)chunk * groups_all + (i - chunk * a.pieces)];
+        };
+        auto count = [&](int i) {
+            const int chunk = a.pieces > 1 ? a.by_pieces.div(i) : i, piece = i - chunk * a.pieces;
+            const int width = a.pieces > 1 ? min(a.slab, a.c - piece * a.slab) : a.c;
+            return (float)min(a.chunk_rows, p.len - chunk * a.chunk_rows) * (float)width;
+        };
+        float2 keep[kGnBatch];
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k) keep[k] = get(min(lane + k * w, total - 1));
+        const float m0 = get(0).x;
+        float cnt = 0.0f, sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k)
+            if (lane + k * w < total) {
+                const float n = count(lane + k * w);
+                cnt += n;
+                sum += n * (keep[k].x - m0);
+            }
+        for (int i = lane + kGnBatch * w; i < total; i += w) {
+            const float n = count(i);
+            cnt += n;
+            sum += n * (get(i).x - m0);
+        }
+        cnt = lane_sum(cnt, w);
+        const float d = lane_sum(sum, w) / cnt;
+        float m2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kGnBatch; ++k)
+            if (lane + k * w < total) {
+                const float t = (keep[k].x - m0) - d;
+                m2 += keep[k].y + count(lane + k * w) * t * t;
+            }
+        for (int i = lane + kGnBatch * w; i < total; i += w) {
+            const float2 v = get(i);
+            const float t = (v.x - m0) - d;
+            m2 += v.y + count(i) * t * t;
+        }
+        m2 = lane_sum(m2, w);
+        if (lane == 0) stat[g] = make_float2(m0 + d, 1.0f / sqrtf(m2 / cnt + a.eps));
+    }
+}
+
+template <typename TX, typename TY, int VEC, int ACT>
+__global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
+    __shared__ float2 stat[kGnThreads * VEC];    // a slab's groups: at most its channels
+    int chunk;
+    const int rest = a.by_chunks.div((int)blockIdx.x, chunk);
+    const GnPlace<kGnThreads, VEC> p(a, rest);
+    const int64_t r0 = chunk * a.chunk_rows, r1 = min(a.N, r0 + a.chunk_rows);
+    GnChannels<VEC> c;
+    float A[VEC] = {}, S[VEC] = {};
+    if (r0 < p.len) {
+        gn_channels<TX, VEC, true>(a, p, c);
+        gn_join_chunks(a, p, stat);
+        __syncthreads();
+        if (p.on) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) gn_factor(stat[c.grp[k]], c.gamma[k], c.beta[k], A[k], S[k]);
+        }
+    }
+    if (!p.on) return;
+    const TX* __restrict__ xp = static_cast<const TX*>(a.x) + p.b * a.N * a.ldx + p.ch0 + p.vec * VEC;
+    TY* __restrict__ yp = static_cast<TY*>(a.y) + p.b * a.N * a.ldy + p.ch0 + p.vec * VEC;
+    const int64_t valid = min(r1, p.len);
+    int64_t r = r0 + p.slot;
+#pragma unroll 4
+    for (; r < valid; r += p.slots) {
+        const GnVec<TX, VEC> w = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + r * a.ldx);
+        GnVec<TY, VEC> o;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) o.e[k] = gn_round<TY>(gn_act<ACT>(fmaf(gn_float(w.e[k]) - c.ref[k], A[k], S[k])));
+        gn_store(yp + r * a.ldy, o);
+    }
+    for (; r < r1; r += p.slots) gn_store(yp + r * a.ldy, GnVec<TY, VEC>{});
+}
+
+// Sums over the workgroup of each group's values: a thread's per channel,
+// then over the rows of its wave, then over waves and channels.  A wave holds
+// whole copies of the vectors' lanes (nvp of them, a power of two) or the
+// workgroup holds rows of several waves.
+template <int VEC, typename P>
+__device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int nvp, float (&v)[VEC], float* ent,
+                                              float* res) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v[k] = wave_sum_from(v[k], nvp);
+    const int slots = nvp <= 64 ? kGnOneThreads / 64 : p.slots;
+    const int slot = nvp <= 64 ? wave : p.slot;
+    __syncthreads();
+    if (p.vec * VEC < p.width && (nvp > 64 || lane < nvp))
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) ent[slot * p.width + p.vec * VEC + k] = v[k];
+    __syncthreads();
+    const int w = gn_lanes<kGnOneThreads>(p.groups, slots * a.c);
+    int we = 1;
+    while (we < w && we < a.c) we *= 2;
+    const int lw = __builtin_ctz(w), le = __builtin_ctz(we);
+    const int l = threadIdx.x & (w - 1), ws = w >> le, s0 = l >> le, e0 = l & (we - 1);
+    for (int g = threadIdx.x >> lw; g < p.groups; g += kGnOneThreads >> lw) {
+        float sum = 0.0f;
+        for (int s = s0; s < slots; s += ws)
+            for (int e = e0; e < a.c; e += we) sum += ent[s * p.width + g * a.c + e];
+        sum = lane_sum(sum, w);
+        if (l == 0) res[g] = sum;
+    }
+    __syncthreads();
+}
+
+// One launch: the slab's valid rows stay in registers between the
+// statistics and the output, so the variance is taken about the mean.
+template <typename TX, typename TY, int VEC, int ACT>
+__global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
+    __shared__ float ent[kGnOneThreads * VEC];   // [slots][width], at most a value for each thread and channel
+    __shared__ float sums[kGnOneThreads * VEC];  // a slab's groups: at most its channels
+    const int nv = (int)a.by_nv.d;
+    const int shift = nv > 1 ? 32 - __builtin_clz(nv - 1) : 0, nvp = 1 << shift;     // lanes of a row
+    GnPlace<kGnOneThreads, VEC> p(a, (int)blockIdx.x);
+    p.slots = kGnOneThreads >> shift;
+    p.slot = threadIdx.x >> shift;
+    p.vec = threadIdx.x & (nvp - 1);
+    p.on = p.vec < nv;
+    const int nrows = (int)p.len;
+    const int mine = p.on && p.slot < nrows ? ((nrows - 1 - p.slot) >> (__builtin_ctz(kGnOneThreads) - shift)) + 1 : 0;
+    const TX* __restrict__ xp = static_cast<const TX*>(a.x) + (p.b * a.N + p.slot) * a.ldx + p.ch0 + p.vec * VEC;
+    TY* __restrict__ yp = static_cast<TY*>(a.y) + (p.b * a.N + p.slot) * a.ldy + p.ch0 + p.vec * VEC;
+    GnChannels<VEC> c;
+    gn_channels<TX, VEC, true>(a, p, c);
+    GnVec<TX, VEC> w[kGnKeep];
+#pragma unroll
+    for (int i = 0; i < kGnKeep; ++i)
+        if (i < mine) w[i] = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + (int64_t)i * p.slots * a.ldx);
+    float A[VEC] = {}, S[VEC] = {};
+    if (nrows > 0) {
+        const float inv = 1.0f / ((float)nrows * (float)a.c);
+        float v[VEC] = {}, mean[VEC];
+#pragma unroll
+        for (int i = 0; i < kGnKeep; ++i)
+            if (i < mine)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) v[k] += gn_float(w[i].e[k]) - c.ref[k];
+        gn_group_sums<VEC>(a, p, nvp, v, ent, sums);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            mean[k] = sums[c.grp[k]] * inv;
+            v[k] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kGnKeep; ++i)
+            if (i < mine)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const float d = (gn_float(w[i].e[k]) - c.ref[k]) - mean[k];
+                    v[k] = fmaf(d, d, v[k]);
+                }
+        gn_group_sums<VEC>(a, p, nvp, v, ent, sums);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            if (mine > 0)
+                gn_factor(make_float2(mean[k], 1.0f / sqrtf(sums[c.grp[k]] * inv + a.eps)), c.gamma[k], c.beta[k], A[k],
+                          S[k]);
+    }
+    if (!p.on) return;
+#pragma unroll
+    for (int i = 0; i < kGnKeep; ++i)
+        if (i < mine) {
+            GnVec<TY, VEC> o;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                o.e[k] = gn_round<TY>(gn_act<ACT>(fmaf(gn_float(w[i].e[k]) - c.ref[k], A[k], S[k])));
+            *reinterpret_cast<GnVec<TY, VEC>*>(yp + (int64_t)i * p.slots * a.ldy) = o;
+        }
+    for (int64_t r = (int64_t)p.slot + (int64_t)mine * p.slots; r < a.N; r += p.slots)
+        *reinterpret_cast<GnVec<TY, VEC>*>(yp + (r - p.slot) * a.ldy) = GnVec<TY, VEC>{};
+}
+
+// How a call is cut.
+struct GnPlan {
+    bool one;
+    int slab, slabs, pieces, chunks;
+    int64_t chunk_rows;
+};
+
+int64_t gn_gcd(int64_t a, int64_t b) { return b ? gn_gcd(b, a % b) : a; }
+
+GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
+    GnPlan p;
+    const int c = C / G;
+    p.pieces = 1;
+    p.chunks = 1;
+    p.chunk_rows = N;
+    // the shortest run of whole groups and whole vectors (C is a multiple of both)
+    const int64_t base = (int64_t)c / gn_gcd(c, vec) * vec;
+    const int64_t room = (int64_t)kGnOneThreads * kGnKeep;
+    auto fits = [&](int64_t slab) {
+        int64_t nvp = 1;               // lanes of a row, a power of two
+        while (nvp < slab / vec) nvp *= 2;
+        return nvp <= kGnOneThreads && ceil_div(N, kGnOneThreads / nvp) <= kGnKeep;
+    };
+    p.one = base <= C && N <= room && fits(base);
+    if (p.one) {
+        // longer runs read whole lines; not past 256 bytes, nor below a workgroup for each compute unit
+        int64_t slab = base;
+        while (2 * slab <= C && C % (2 * slab) == 0 && 2 * slab / vec <= 16 && fits(2 * slab) &&
+               B * (C / (2 * slab)) >= 256)
+            slab *= 2;
+        p.slab = (int)slab;
+        p.slabs = (int)(C / slab);
+        return p;
+    }
+    const int64_t most = (int64_t)kGnThreads * vec;
+    if (base <= most && base <= C) {
+        int64_t slab = base;
+        while (slab + base <= most && slab + base <= C) slab += base;
+        p.slab = (int)slab;
+        p.slabs = (int)ceil_div(C, slab);
+    } else {
+        // a group wider than the threads' vectors, in pieces (c is then a multiple of vec, or vec is 1)
+        p.slab = (int)most;
+        p.pieces = (int)ceil_div(c, most);
+        p.slabs = G * p.pieces;
+    }
+    const int64_t slots = std::max<int64_t>(1, kGnThreads / ceil_div(std::min<int64_t>(p.slab, C), vec));
+    // at most 128 chunks of a cloud, which every workgroup of the second launch joins, while a thread's chain of sums
+    // stays within 128 rows; at least 8 rows a thread
+    const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, kGnBlocks / std::max<int64_t>(1, B * p.slabs)));
+    int64_t rows = std::max<int64_t>(ceil_div(N, want), 8 * slots);
+    rows = std::max<int64_t>(std::min<int64_t>(rows, 128 * slots), ceil_div(N, 4096));
+    p.chunk_rows = rows;
+    p.chunks = (int)ceil_div(N, rows);
+    return p;
+}
+
+size_t group_norm_ws(const GnPlan& p, int64_t B, int G) {
+    return p.one ? 0 : ((size_t)(B * p.chunks * G * p.pieces) * 8 + 15) / 16 * 16;
+}
+
+// Widest vector: 16 bytes of x where C allows them, else single values.
+int group_norm_vec(int C, int G, int x_dtype) {
+    const int vec = x_dtype == MESORASI_F32 ? 4 : 8;
+    const int c = C / G;
+    // whole vectors in a row, and in a group where it is cut into pieces
+    return C % vec == 0 && (c % vec == 0 || c <= 64) ? vec : 1;
+}
+
+template <typename TX, typename TY, int VEC, int ACT>
+void launch_group_norm(const GnArgs& a, const GnPlan& p, hipStream_t s) {
+    const int64_t blocks = a.B * a.slabs * a.chunks;
+    if (p.one) {
+        gn_one_kernel<TX, TY, VEC, ACT><<<dim3((unsigned)blocks), dim3(kGnOneThreads), 0, s>>>(a);
+        return;
+    }
+    gn_parts_kernel<TX, VEC><<<dim3((unsigned)blocks), dim3(kGnThreads), 0, s>>>(a);
+    gn_apply_kernel<TX, TY, VEC, ACT><<<dim3((unsigned)blocks), dim3(kGnThreads), 0, s>>>(a);
+}
+
+template <typename TX, typename TY, int VEC>
+void launch_group_norm(const GnArgs& a, const GnPlan& p, hipStream_t s) {
+    switch (a.act) {
+        case MESORASI_ACT_RELU: launch_group_norm<TX, TY, VEC, MESORASI_ACT_RELU>(a, p, s); break;
+        case MESORASI_ACT_SILU: launch_group_norm<TX, TY, VEC, MESORASI_ACT_SILU>(a, p, s); break;
+        case MESORASI_ACT_GELU: launch_group_norm<TX, TY, VEC, MESORASI_ACT_GELU>(a, p, s); break;
+        default: launch_group_norm<TX, TY, VEC, MESORASI_ACT_NONE>(a, p, s); break;
     }
 }
 
@@ -88,8 +585,17 @@ __global__ __launch_bounds__(kGnThreads) void group_norm_kernel(const TX* __rest
 
 using namespace meso;
 
+static bool group_norm_sizes_ok(int64_t B, int64_t N, int32_t C, int32_t G) {
+    return B >= 1 && N >= 1 && C >= 1 && G >= 1 && C % G == 0 && C <= MESORASI_MAX_C_NORM && N <= 0x7fffffff &&
+           B <= 0x7fffffff / G;
+}
+
 extern "C" size_t mesorasi_group_norm_workspace(int64_t B, int64_t N, int32_t C, int32_t G, int32_t x_dtype) {
-    return 0;
+    if (!group_norm_sizes_ok(B, N, C, G) || (x_dtype != MESORASI_F32 && x_dtype != MESORASI_BF16)) return 0;
+    // rows of any alignment: the larger of both vector widths' needs
+    const size_t a = group_norm_ws(plan_group_norm(B, N, C, G, 1), B, G);
+    const int vec = group_norm_vec(C, G, x_dtype);
+    return std::max(a, group_norm_ws(plan_group_norm(B, N, C, G, vec), B, G));
 }
 
 extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype, int64_t B, int64_t N, int32_t C,
@@ -109,17 +615,32 @@ extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype,
                  "mesorasi_group_norm: B = %lld, N = %lld, C = %d", (long long)B, (long long)N, C);
     if (B == 0 || N == 0) return MESORASI_OK;
     MESO_REQUIRE(x && y, MESORASI_EINVAL, "mesorasi_group_norm: NULL x or y");
+    const int ex = x_dtype == MESORASI_F32 ? 4 : 2, ey = y_dtype == MESORASI_F32 ? 4 : 2;
+    int vec = group_norm_vec(C, G, x_dtype);
+    if (vec > 1 && !(ld_x % vec == 0 && ld_y % vec == 0 && aligned(x, vec * ex) && aligned(y, std::min(16, vec * ey))))
+        vec = 1;
+    const GnPlan p = plan_group_norm(B, N, C, G, vec);
+    const size_t need = group_norm_ws(p, B, G);
+    MESO_REQUIRE(need == 0 || (ws && ws_bytes >= need), MESORASI_EWORKSPACE,
+                 "mesorasi_group_norm: workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+    MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_group_norm: ws is not 16-byte aligned");
+    MESO_REQUIRE(B * p.slabs <= 0x7fffffff / p.chunks, MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
+                 (long long)B, (long long)N);
+    const GnArgs a = {x, y, lens, gamma, beta, static_cast<float2*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,
+                      p.slab, p.slabs, p.pieces, p.chunks, p.chunk_rows, FastDiv(p.chunks), FastDiv(p.slabs),
+                      FastDiv(p.pieces), FastDiv(C / G), FastDiv((unsigned)p.chunk_rows), FastDiv((unsigned)ceil_div(p.slab, vec))};
     hipStream_t s = as_stream(stream);
-    const dim3 grid((unsigned)(B * G)), block(kGnThreads);
-#define MESO_GN(TX, TY)                                                                                          \
-    group_norm_kernel<TX, TY><<<grid, block, 0, s>>>(static_cast<const TX*>(x), ld_x, N, C, G, lens, gamma, beta, \
-                                                     eps, act, static_cast<TY*>(y), ld_y)
+#define MESO_GN(TX, TY, V)                                              \
+    do {                                                                \
+        if (vec > 1) launch_group_norm<TX, TY, V>(a, p, s);             \
+        else launch_group_norm<TX, TY, 1>(a, p, s);                     \
+    } while (0)
     if (x_dtype == MESORASI_F32) {
-        if (y_dtype == MESORASI_F32) MESO_GN(float, float);
-        else MESO_GN(float, uint16_t);
+        if (y_dtype == MESORASI_F32) MESO_GN(float, float, 4);
+        else MESO_GN(float, uint16_t, 4);
     } else {
-        if (y_dtype == MESORASI_F32) MESO_GN(uint16_t, float);
-        else MESO_GN(uint16_t, uint16_t);
+        if (y_dtype == MESORASI_F32) MESO_GN(uint16_t, float, 8);
+        else MESO_GN(uint16_t, uint16_t, 8);
     }
 #undef MESO_GN
     return after_launch("mesorasi_group_norm");
