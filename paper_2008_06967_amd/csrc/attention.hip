@@ -37,77 +37,6 @@ struct AttnArgs {
     float* part;        // splits > 1: [pair, split, row, Dp] sums, then [pair, split, row, 2] maximum and sum
 };
 
-template <typename T>
-__device__ __forceinline__ float at_load(const T* p) {
-    if constexpr (sizeof(T) == 4)
-        return *p;
-    else
-        return bf16_to_f32(*p);
-}
-
-// One wave per query and head: 64 sources at a time, a source per lane for
-// the scores, a channel (two for D > 64) per lane for the output.
-template <typename T>
-__global__ __launch_bounds__(64) void attention_kernel(AttnArgs a, int64_t total) {
-    __shared__ float qs[MESORASI_MAX_D_ATTN];
-    __shared__ float ps[64];
-    const int lane = threadIdx.x;
-    const int64_t e = blockIdx.x;
-    const int h = (int)(e % a.Hq);
-    const int64_t n = e / a.Hq % a.Nq, b = e / a.Hq / a.Nq;
-    const int kvh = h / (a.Hq / a.Hkv);
-    const T* q = static_cast<const T*>(a.q) + b * a.qb + n * a.ql + h * a.qh;
-    const T* k = static_cast<const T*>(a.k) + b * a.kb + kvh * a.kh;
-    const T* v = static_cast<const T*>(a.v) + b * a.vb + kvh * a.vh;
-    T* o = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
-    const int64_t len = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
-    const uint8_t* mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
-    for (int c = lane; c < a.D; c += 64) qs[c] = at_load(q + c) * a.scale;
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int64_t j0 = 0; j0 < len; j0 += 64) {
-        const int64_t j = j0 + lane;
-        const bool ok = j < len && (!mask || mask[j]);
-        float s = -INFINITY;
-        if (ok) {
-            s = 0.0f;
-            for (int c = 0; c < a.D; ++c) s = fmaf(qs[c], at_load(k + j * a.kl + c), s);
-        }
-        float mt = s;
-        for (int w = 32; w; w >>= 1) mt = fmaxf(mt, __shfl_xor(mt, w));
-        const float mn = fmaxf(m, mt);
-        const float base = mn == -INFINITY ? 0.0f : mn;
-        const float p = expf(s - base);
-        float lt = p;
-        for (int w = 32; w; w >>= 1) lt += __shfl_xor(lt, w);
-        const float f = expf(m - base);
-        l = l * f + lt;
-        o0 *= f;
-        o1 *= f;
-        m = mn;
-        __syncthreads();
-        ps[lane] = p;
-        __syncthreads();
-        const uint64_t okm = ballot(ok);
-        for (int i = 0; i < 64; ++i) {
-            if (!((okm >> i) & 1)) continue;
-            const T* vr = v + (j0 + i) * a.vl;
-            if (lane < a.D) o0 = fmaf(ps[i], at_load(vr + lane), o0);
-            if (lane + 64 < a.D) o1 = fmaf(ps[i], at_load(vr + lane + 64), o1);
-        }
-    }
-    const float r = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    for (int i = 0; i < 2; ++i) {
-        const int c = lane + 64 * i;
-        if (c >= a.D) continue;
-        const float w = (i ? o1 : o0) * r;
-        if constexpr (sizeof(T) == 4)
-            o[c] = w;
-        else
-            o[c] = f32_to_bf16_any(w);
-    }
-}
-
 
 // ---------------------------------------------------------------------------
 // bf16
@@ -156,6 +85,47 @@ __device__ __forceinline__ uint32_t at_pack(float a, float b) {
 __device__ __forceinline__ uint64_t at_count_bits(int64_t j0, int64_t end) {
     const int64_t r = end - j0;
     return r >= 64 ? ~0ull : r <= 0 ? 0ull : (1ull << r) - 1;
+}
+
+// The waves that share 32 rows join: sh [W][Dp][32 rows] their sums, sm [W][32]
+// maxima and [W][32] sums of weights.
+template <typename T, int Dp, int W>
+__device__ __forceinline__ void at_join_waves(const AttnArgs& a, const float* sh, const float* sm, int row0,
+                                              int64_t pair, int split, int64_t b, int kvh, int g) {
+    const int tid = threadIdx.x, r = tid & 31, row = row0 + r;
+    if (row >= a.rows) return;
+    float mm[W], M = -INFINITY, L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) M = fmaxf(M, mm[w] = sm[w * 32 + r]);
+    const float base = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        mm[w] = at_exp2(mm[w] - base);
+        L += mm[w] * sm[(W + w) * 32 + r];
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const int n = row / g, h = kvh * g + (row - n * g);
+    T* op = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+    const int64_t pr = (pair * a.splits + split) * a.rows + row;
+    for (int d = tid >> 5; d < a.D; d += 2 * W) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += mm[w] * sh[(w * Dp + d) * 32 + r];
+        if (a.splits > 1) {
+            a.part[pr * Dp + d] = v;
+        } else {
+            v *= inv;
+            if constexpr (sizeof(T) == 4)
+                op[d] = v;
+            else
+                op[d] = f32_to_bf16_any(v);
+        }
+    }
+    if (a.splits > 1 && tid < 32) {
+        float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * Dp;
+        pm[2 * pr] = M;
+        pm[2 * pr + 1] = L;
+    }
 }
 
 // The product taken transposed, S^T = K Q^T and O^T = V^T P^T on
@@ -440,35 +410,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
             sm[128 + wave * 32 + col] = l[0];
         }
         __syncthreads();
-        const int r = tid & 31, row = row0 + r;
-        if (row >= a.rows) return;
-        float mm[4], M = -INFINITY, L = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, mm[w] = sm[w * 32 + r]);
-        const float base = M == -INFINITY ? 0.0f : M;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            mm[w] = at_exp2(mm[w] - base);
-            L += mm[w] * sm[128 + w * 32 + r];
-        }
-        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-        const int n = row / g, h = kvh * g + (row - n * g);
-        uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
-        const int64_t pr = (pair * a.splits + split) * a.rows + row;
-        for (int d = tid >> 5; d < a.D; d += kAtThreads / 32) {
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) v += mm[w] * sh[(w * Dp + d) * 32 + r];
-            if (a.splits > 1)
-                a.part[pr * Dp + d] = v;
-            else
-                op[d] = f32_to_bf16_any(v * inv);
-        }
-        if (a.splits > 1 && tid < 32) {
-            float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * Dp;
-            pm[2 * pr] = M;
-            pm[2 * pr + 1] = L;
-        }
+        at_join_waves<uint16_t, Dp, 4>(a, sh, sm, row0, pair, split, b, kvh, g);
     } else {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
@@ -493,6 +435,330 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
                     }
                 }
         }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// fp32
+// ---------------------------------------------------------------------------
+
+// v = hi + mid + lo, each in bf16: 8 bits each of a float's 24, with nothing
+// left over (values that bf16 rounds to infinity, above 3.39e38, aside).
+struct AtSplit {
+    uint32_t hi, mid, lo;            // of two values
+};
+
+__device__ __forceinline__ AtSplit at_split(float a, float b) {
+    AtSplit s;
+    s.hi = at_pack(a, b);
+    a -= __uint_as_float(s.hi << 16);
+    b -= __uint_as_float(s.hi & 0xffff0000u);
+    s.mid = at_pack(a, b);
+    a -= __uint_as_float(s.mid << 16);
+    b -= __uint_as_float(s.mid & 0xffff0000u);
+    s.lo = at_pack(a, b);
+    return s;
+}
+
+// Eight values into one operand of each part.
+__device__ __forceinline__ void at_split8(const float (&f)[8], uint4 (&w)[3]) {
+    AtSplit s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = at_split(f[2 * i], f[2 * i + 1]);
+    w[0] = make_uint4(s[0].hi, s[1].hi, s[2].hi, s[3].hi);
+    w[1] = make_uint4(s[0].mid, s[1].mid, s[2].mid, s[3].mid);
+    w[2] = make_uint4(s[0].lo, s[1].lo, s[2].lo, s[3].lo);
+}
+
+// A product of split operands: the six partial products down to 2^-16 of it,
+// the small ones first; the three left out are below 2^-24.
+__device__ __forceinline__ f32x16 at_mfma6(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 c) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2], b[0], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[2], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[1], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[0], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[1], c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[0], c, 0, 0, 0);
+}
+
+// The bf16 kernel's scheme with every operand in three bf16 parts and six
+// matrix instructions a product: 419 TFLOP/s at most instead of the fp32
+// instruction's 157.  K and V are split once a tile, on their way to LDS (the
+// next tile's rows wait in registers); Q once, the weights where they form.
+// Waves: four with 32 rows of their own; or, sharing 32 rows (KS), four, or
+// two above 64 channels, where the parts of more sources would not fit LDS.
+template <int DB, bool KS>
+struct AtF32 {
+    static constexpr int kWaves = KS && DB > 2 ? 2 : 4;
+    static constexpr int KT = KS ? 32 * kWaves : DB > 2 ? 32 : 64;      // sources of a tile
+    static constexpr int NB = KS ? 1 : KT / 32;
+    static constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;           // 16-byte chunks of a row of one part
+    static constexpr int kPart = KT * CH * 16;                          // bytes of one part of a tile
+    static constexpr int kUnits = KT * CH / (64 * kWaves);              // chunks of K (and of V) a thread stages
+    static constexpr int kJoin = KS ? kWaves * (32 * DB * 32 + 2 * 32) * 4 : 0;
+    static constexpr int kLds = 6 * kPart > kJoin ? 6 * kPart : kJoin;
+};
+
+template <int DB, bool KS, bool GEN>
+__global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) void attention_f32_kernel(AttnArgs a) {
+    using P = AtF32<DB, KS>;
+    constexpr int CH = P::CH, KT = P::KT, NB = P::NB, kThreads = 64 * P::kWaves;
+    extern __shared__ __align__(16) char lds[];              // K's three parts, then V's
+
+    const int64_t lb = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (lb >= a.blocks) return;
+    const int split = (int)(lb % a.splits);
+    const int64_t rest = lb / a.splits;
+    const int tile0 = (int)(rest % a.row_tiles);
+    const int64_t pair = rest / a.row_tiles;
+    const int64_t b = pair / a.Hkv;
+    const int kvh = (int)(pair - b * a.Hkv);
+    const int g = a.Hq / a.Hkv;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int half = lane >> 5, col = lane & 31;
+
+    const float* __restrict__ kp = static_cast<const float*>(a.k) + b * a.kb + kvh * a.kh;
+    const float* __restrict__ vp = static_cast<const float*>(a.v) + b * a.vb + kvh * a.vh;
+    const uint8_t* __restrict__ mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
+    int64_t end = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
+    int64_t begin = 0;
+    if (a.splits > 1) {
+        const int64_t per = ((end + a.splits - 1) / a.splits + KT - 1) / KT * KT;
+        begin = min(end, split * per);
+        end = min(end, begin + per);
+    }
+    const int tiles = (int)((end - begin + KT - 1) / KT);
+
+    const float c0 = a.scale * 1.44269504088896340736f;
+    const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
+    const float qmul = c0 == 0.0f ? 0.0f : c0 < 0.0f ? -1.0f : 1.0f;
+
+    auto read8 = [&](const float* p, int d0, bool ok, float (&f)[8]) {
+        if constexpr (GEN) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = ok && d0 + e < a.D ? p[d0 + e] : 0.0f;
+        } else {                     // D is a multiple of 4
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (ok && d0 + e < a.D) v = *reinterpret_cast<const float4*>(p + d0 + e);
+                f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
+            }
+        }
+    };
+
+    // the wave's queries: operand B, channel 16 s + 8 half + e
+    const int row = tile0 * (KS ? 32 : 128) + (KS ? 0 : wave * 32) + col;
+    bf16x8 qf[2 * DB][3];
+    {
+        const int r = min(row, a.rows - 1), n = r / g, h = kvh * g + (r - n * g);
+        const float* qp = static_cast<const float*>(a.q) + b * a.qb + n * a.ql + h * a.qh;
+#pragma unroll
+        for (int s = 0; s < 2 * DB; ++s) {
+            float f[8];
+            uint4 w[3];
+            read8(qp, 16 * s + 8 * half, true, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = qmul == 0.0f ? 0.0f : f[e] * qmul;
+            at_split8(f, w);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) qf[s][i] = __builtin_bit_cast(bf16x8, w[i]);
+        }
+    }
+
+    auto valid_bits = [&](int t, uint64_t (&bits)[(KT + 63) / 64]) {
+#pragma unroll
+        for (int i = 0; i < (KT + 63) / 64; ++i) {
+            const int64_t j = begin + (int64_t)t * KT + 64 * i;
+            bits[i] = at_count_bits(j, end);
+            if (mask) bits[i] &= ballot(j + lane < end && mask[j + lane]);
+        }
+    };
+    float kr[P::kUnits][8], vr[P::kUnits][8];
+    auto fetch = [&](int t, const uint64_t (&bits)[(KT + 63) / 64]) {
+        const int64_t j0 = begin + (int64_t)t * KT;
+#pragma unroll
+        for (int i = 0; i < P::kUnits; ++i) {
+            const int p = i * kThreads + tid, r = p / CH, ch = (p % CH) ^ at_swz<CH>(r);
+            const bool ok = (bits[KT > 64 ? r >> 6 : 0] >> (r & 63)) & 1;
+            read8(kp + (j0 + r) * a.kl, 8 * ch, ok, kr[i]);
+            read8(vp + (j0 + r) * a.vl, 8 * ch, ok, vr[i]);
+        }
+    };
+    auto store = [&]() {
+#pragma unroll
+        for (int i = 0; i < P::kUnits; ++i) {
+            uint4 w[3], x[3];
+            at_split8(kr[i], w);
+            at_split8(vr[i], x);
+            char* d = lds + (i * kThreads + tid) * 16;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                *reinterpret_cast<uint4*>(d + k * P::kPart) = w[k];
+                *reinterpret_cast<uint4*>(d + (3 + k) * P::kPart) = x[k];
+            }
+        }
+    };
+
+    f32x16 oacc[DB];
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
+
+    const int swk = at_swz<CH>(col);
+    const int vi = lane & 15, vg = (lane >> 4) & 1;
+    const int vrow = 4 * half + (vi >> 2);
+    const int vch = 2 * vg + ((vi & 3) >> 1), vin = 8 * (vi & 1);
+
+    uint64_t cur[(KT + 63) / 64], nxt[(KT + 63) / 64] = {};
+    if (tiles > 0) {
+        valid_bits(0, cur);
+        fetch(0, cur);
+    }
+    for (int t = 0; t < tiles; ++t) {
+        __syncthreads();             // the tile before has been read
+        store();
+        __syncthreads();
+        if (t + 1 < tiles) {
+            valid_bits(t + 1, nxt);
+            fetch(t + 1, nxt);
+        }
+        const char* tk = lds;
+        const char* tv = lds + 3 * P::kPart;
+
+        f32x16 s[NB];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const char* base = tk + (32 * (KS ? wave : kb) + col) * CH * 16;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kb][r] = 0.0f;
+            bf16x8 kf[2][3];
+            auto read_k = [&](int st) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    kf[st & 1][i] =
+                        *reinterpret_cast<const bf16x8*>(base + i * P::kPart + (((2 * st + half) ^ swk) << 4));
+            };
+            read_k(0);
+#pragma unroll
+            for (int st = 0; st < 2 * DB; ++st) {
+                if (st + 1 < 2 * DB) read_k(st + 1);
+                s[kb] = at_mfma6(kf[st & 1], qf[st], s[kb]);
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int blk = KS ? wave : kb;
+            const uint32_t w32 = (uint32_t)(cur[KT > 64 ? blk >> 1 : 0] >> (32 * (blk & 1)));
+            if (w32 != 0xffffffffu) {
+                const uint32_t w = w32 >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] = (w >> (8 * (r / 4) + r % 4)) & 1 ? s[kb][r] : -INFINITY;
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+        float lo;
+        const float hi = at_other_half(mx, lo);
+        mx = fmaxf(lo, hi) * c;
+        if (ballot(mx > m + 8.0f)) {
+            const float mn = fmaxf(m, mx);
+            const float f = mn == -INFINITY ? 1.0f : at_exp2(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int blk = KS ? wave : kb;
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                // this step's 16 weights, sources 16 st + 8 (e / 4) + 4 half + e % 4
+                float pf[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[e] = at_exp2(fmaf(s[kb][8 * st + e], c, -base));
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) l += pf[e] + pf[e + 1];
+                uint4 pw[3];
+                at_split8(pf, pw);
+                bf16x8 pb[3];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) pb[i] = __builtin_bit_cast(bf16x8, pw[i]);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    bf16x8 vf[3];
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+                        s16x4 v[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int vr0 = 32 * blk + 16 * st + 8 * e + vrow;
+                            const int ch = (4 * d + vch) ^ (at_swz<CH>(vrow) | 2 * e);
+                            v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (lds_s16x4)(tv + i * P::kPart + vr0 * CH * 16 + (ch << 4) + vin));
+                        }
+                        const uint4 vw =
+                            make_uint4(__builtin_bit_cast(uint2, v[0]).x, __builtin_bit_cast(uint2, v[0]).y,
+                                       __builtin_bit_cast(uint2, v[1]).x, __builtin_bit_cast(uint2, v[1]).y);
+                        vf[i] = __builtin_bit_cast(bf16x8, vw);
+                    }
+                    oacc[d] = at_mfma6(vf, pb, oacc[d]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < (KT + 63) / 64; ++i) cur[i] = nxt[i];
+    }
+
+    {
+        float lo;
+        const float hi = at_other_half(l, lo);
+        l = lo + hi;
+    }
+    if constexpr (KS) {
+        constexpr int Dp = 32 * DB, W = P::kWaves;
+        float* sh = reinterpret_cast<float*>(lds);
+        float* sm = sh + W * Dp * 32;
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                sh[(wave * Dp + 32 * d + 8 * (r / 4) + 4 * half + r % 4) * 32 + col] = oacc[d][r];
+        if (half == 0) {
+            sm[wave * 32 + col] = m;
+            sm[(W + wave) * 32 + col] = l;
+        }
+        __syncthreads();
+        at_join_waves<float, Dp, W>(a, sh, sm, tile0 * 32, pair, split, b, kvh, g);
+    } else {
+        if (row >= a.rows) return;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int n = row / g, h = kvh * g + (row - n * g);
+        float* op = static_cast<float*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int d0 = 32 * d + 2 * r + 4 * half;
+                if constexpr (GEN) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (d0 + e < a.D) op[d0 + e] = oacc[d][r + e] * inv;
+                } else if (d0 < a.D) {
+                    *reinterpret_cast<float4*>(op + d0) = make_float4(oacc[d][r] * inv, oacc[d][r + 1] * inv,
+                                                                      oacc[d][r + 2] * inv, oacc[d][r + 3] * inv);
+                }
+            }
     }
 }
 
@@ -564,12 +830,12 @@ struct AttnPlan {
 
 constexpr int kAtCus = 256;
 
-AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int D) {
+AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int D, int dtype) {
     AttnPlan p;
     const int64_t pairs = B * Hkv, rows = Nq * (Hq / Hkv);
     p.Dp = (D + 31) / 32 * 32;
     p.splits = 1;
-    if (D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
+    if (dtype == MESORASI_BF16 && D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
         p.qb = 2;
     else if (pairs * ceil_div(rows, 128) >= kAtCus * 3 / 4)
         p.qb = 1;
@@ -619,6 +885,31 @@ int launch_attention_bf16(const AttnArgs& a, int qb, unsigned grid, hipStream_t 
     }
 }
 
+template <int DB, bool KS, bool GEN>
+int launch_attention_f32(const AttnArgs& a, unsigned grid, hipStream_t s) {
+    using P = AtF32<DB, KS>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_f32_kernel<DB, KS, GEN>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, P::kLds);
+    MESO_REQUIRE(attr == hipSuccess, MESORASI_EHIP, "mesorasi_cross_attention: LDS size attribute: %s",
+                 hipGetErrorString(attr));
+    attention_f32_kernel<DB, KS, GEN><<<dim3(grid), dim3(64 * P::kWaves), P::kLds, s>>>(a);
+    return MESORASI_OK;
+}
+
+template <bool GEN>
+int launch_attention_f32(const AttnArgs& a, int qb, unsigned grid, hipStream_t s) {
+    switch ((a.D + 31) / 32 * 2 + (qb == 0)) {
+        case 2: return launch_attention_f32<1, false, GEN>(a, grid, s);
+        case 3: return launch_attention_f32<1, true, GEN>(a, grid, s);
+        case 4: return launch_attention_f32<2, false, GEN>(a, grid, s);
+        case 5: return launch_attention_f32<2, true, GEN>(a, grid, s);
+        case 6: return launch_attention_f32<3, false, GEN>(a, grid, s);
+        case 7: return launch_attention_f32<3, true, GEN>(a, grid, s);
+        case 8: return launch_attention_f32<4, false, GEN>(a, grid, s);
+        default: return launch_attention_f32<4, true, GEN>(a, grid, s);
+    }
+}
+
 }  // namespace
 
 }  // namespace meso
@@ -630,8 +921,8 @@ extern "C" size_t mesorasi_cross_attention_workspace(int64_t B, int64_t Nq, int6
     if (B < 1 || Nq < 1 || Nk < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || D < 1 || D > MESORASI_MAX_D_ATTN ||
         Nk > 0x7fffffff - 1023 || Nq > (0x7fffffff - 1023) / (Hq / Hkv) || B > 0x7fffffff / Hkv)
         return 0;
-    if (dtype != MESORASI_BF16) return 0;
-    return attention_ws(plan_attention(B, Nq, Nk, Hq, Hkv, D), Nq * (Hq / Hkv), B * Hkv);
+    if (dtype != MESORASI_BF16 && dtype != MESORASI_F32) return 0;
+    return attention_ws(plan_attention(B, Nq, Nk, Hq, Hkv, D, dtype), Nq * (Hq / Hkv), B * Hkv);
 }
 
 extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_ld, int64_t q_hs, const void* k,
@@ -661,13 +952,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     AttnArgs a = {q, k, v, o, q_bs, q_ld, q_hs, k_bs, k_ld, k_hs, v_bs, v_ld, v_hs, o_bs, o_ld, o_hs,
                   Nq, Nk, mask_ld, Hq, Hkv, D, scale, k_len, k_mask};
     hipStream_t s = as_stream(stream);
-    if (dtype == MESORASI_F32) {
-        const int64_t total = B * Nq * Hq;
-        MESO_REQUIRE(total <= 0x7fffffff, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: size");
-        attention_kernel<float><<<dim3((unsigned)total), dim3(64), 0, s>>>(a, total);
-        return after_launch("mesorasi_cross_attention");
-    }
-    const AttnPlan p = plan_attention(B, Nq, Nk, Hq, Hkv, D);
+    const AttnPlan p = plan_attention(B, Nq, Nk, Hq, Hkv, D, dtype);
     const int64_t pairs = B * Hkv;
     a.rows = (int)(Nq * (Hq / Hkv));
     const size_t need = attention_ws(p, a.rows, pairs);
@@ -682,15 +967,22 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     MESO_REQUIRE(per <= 0x7fffffff / 8, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
                  (long long)p.blocks);
     a.per_xcd = (int)per;
-    // 16-byte chunks of every row, 8-byte pieces of the output
+    // 16-byte pieces of every row, runs of 4 channels of the output
+    const bool f32 = dtype == MESORASI_F32;
     const int64_t st = q_bs | q_ld | q_hs | k_bs | k_ld | k_hs | v_bs | v_ld | v_hs | D;
-    const bool vec = st % 8 == 0 && (o_bs | o_ld | o_hs) % 4 == 0 && aligned(q, 16) && aligned(k, 16) &&
-                     aligned(v, 16) && aligned(o, 8);
-    const int rc = vec ? launch_attention_bf16<false>(a, p.qb, (unsigned)(8 * per), s)
-                       : launch_attention_bf16<true>(a, p.qb, (unsigned)(8 * per), s);
+    const bool vec = st % (f32 ? 4 : 8) == 0 && (o_bs | o_ld | o_hs) % 4 == 0 && aligned(q, 16) && aligned(k, 16) &&
+                     aligned(v, 16) && aligned(o, f32 ? 16 : 8);
+    const unsigned grid = (unsigned)(8 * per);
+    const int rc = f32 ? (vec ? launch_attention_f32<false>(a, p.qb, grid, s) : launch_attention_f32<true>(a, p.qb, grid, s))
+                       : (vec ? launch_attention_bf16<false>(a, p.qb, grid, s)
+                              : launch_attention_bf16<true>(a, p.qb, grid, s));
     if (rc != MESORASI_OK) return rc;
     if (p.splits > 1) {
-        attention_join_kernel<uint16_t><<<dim3((unsigned)(pairs * a.rows)), dim3(kAtThreads), 0, s>>>(a, p.Dp);
+        const dim3 jgrid((unsigned)(pairs * a.rows)), block(kAtThreads);
+        if (f32)
+            attention_join_kernel<float><<<jgrid, block, 0, s>>>(a, p.Dp);
+        else
+            attention_join_kernel<uint16_t><<<jgrid, block, 0, s>>>(a, p.Dp);
     }
     return after_launch("mesorasi_cross_attention");
 }

@@ -555,17 +555,25 @@ def _like(t, x: torch.Tensor, name: str, dtype, shape):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {x.device}")
 
 
+_entry_points: dict = {}
+
+
 def _call(x: torch.Tensor, where: str, *args):
     """The entry point `where` on x's device, on that device's current stream."""
     dev = x.device
     if dev.type != "cuda":
         raise ValueError(f"{where}: tensors must be on a GPU, not on {dev}")
-    fn = getattr(_lib.lib(), "mesorasi_" + where)
-    if dev.index == torch.cuda.current_device():
-        check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
+    fn = _entry_points.get(where)
+    if fn is None:
+        fn = _entry_points[where] = getattr(_lib.lib(), "mesorasi_" + where)
+    i = dev.index
+    if i == torch._C._cuda_getDevice():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(dev):
-            check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if rc:
+        check(rc, where)
 
 
 def _workspace(x: torch.Tensor, need: int, ws):
