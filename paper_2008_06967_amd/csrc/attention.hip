@@ -8,6 +8,7 @@ namespace meso {
 
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -34,6 +35,7 @@ struct AttnArgs {
     int splits;         // workgroups over the sources
     int64_t blocks;     // pairs * row_tiles * splits
     int per_xcd;
+    int Dp;             // channels of a part: D rounded up to 32
     float* part;        // splits > 1: [pair, split, row, Dp] sums, then [pair, split, row, 2] maximum and sum
 };
 
@@ -87,32 +89,32 @@ __device__ __forceinline__ uint64_t at_count_bits(int64_t j0, int64_t end) {
     return r >= 64 ? ~0ull : r <= 0 ? 0ull : (1ull << r) - 1;
 }
 
-// The waves that share 32 rows join: sh [W][Dp][32 rows] their sums, sm [W][32]
-// maxima and [W][32] sums of weights.
-template <typename T, int Dp, int W>
+// The waves that share R rows join: sh [W][Dp][R] their sums, sm [W][R] maxima
+// and [W][R] sums of weights.
+template <typename T, int Dp, int W, int R>
 __device__ __forceinline__ void at_join_waves(const AttnArgs& a, const float* sh, const float* sm, int row0,
                                               int64_t pair, int split, int64_t b, int kvh, int g) {
-    const int tid = threadIdx.x, r = tid & 31, row = row0 + r;
+    const int tid = threadIdx.x, r = tid & (R - 1), row = row0 + r;
     if (row >= a.rows) return;
     float mm[W], M = -INFINITY, L = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) M = fmaxf(M, mm[w] = sm[w * 32 + r]);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, mm[w] = sm[w * R + r]);
     const float base = M == -INFINITY ? 0.0f : M;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         mm[w] = at_exp2(mm[w] - base);
-        L += mm[w] * sm[(W + w) * 32 + r];
+        L += mm[w] * sm[(W + w) * R + r];
     }
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
     const int n = row / g, h = kvh * g + (row - n * g);
     T* op = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
     const int64_t pr = (pair * a.splits + split) * a.rows + row;
-    for (int d = tid >> 5; d < a.D; d += 2 * W) {
+    for (int d = tid / R; d < a.D; d += 64 * W / R) {
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) v += mm[w] * sh[(w * Dp + d) * 32 + r];
+        for (int w = 0; w < W; ++w) v += mm[w] * sh[(w * Dp + d) * R + r];
         if (a.splits > 1) {
-            a.part[pr * Dp + d] = v;
+            a.part[pr * a.Dp + d] = v;
         } else {
             v *= inv;
             if constexpr (sizeof(T) == 4)
@@ -121,10 +123,27 @@ __device__ __forceinline__ void at_join_waves(const AttnArgs& a, const float* sh
                 op[d] = f32_to_bf16_any(v);
         }
     }
-    if (a.splits > 1 && tid < 32) {
-        float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * Dp;
+    if (a.splits > 1 && tid < R) {
+        float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * a.Dp;
         pm[2 * pr] = M;
         pm[2 * pr + 1] = L;
+    }
+}
+
+// A row's part: its two lanes' sums, maximum and sum of weights.
+template <int DB>
+__device__ __forceinline__ void at_write_part(const AttnArgs& a, int64_t pr, const f32x16 (&o)[DB], float m, float l,
+                                              int half) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<float4*>(a.part + pr * a.Dp + 32 * d + 2 * r + 4 * half) =
+                make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+    if (half == 0) {
+        float* pm = a.part + (a.blocks / a.row_tiles) * a.rows * a.Dp;
+        pm[2 * pr] = m;
+        pm[2 * pr + 1] = l;
     }
 }
 
@@ -410,12 +429,16 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
             sm[128 + wave * 32 + col] = l[0];
         }
         __syncthreads();
-        at_join_waves<uint16_t, Dp, 4>(a, sh, sm, row0, pair, split, b, kvh, g);
+        at_join_waves<uint16_t, Dp, 4, 32>(a, sh, sm, row0, pair, split, b, kvh, g);
     } else {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const int row = row0 + 32 * qb + col;
             if (row >= a.rows) continue;
+            if (a.splits > 1) {
+                at_write_part<DB>(a, (pair * a.splits + split) * a.rows + row, oacc[qb], m[qb], l[qb], half);
+                continue;
+            }
             const float inv = l[qb] == 0.0f ? 0.0f : 1.0f / l[qb];
             const int n = row / g, h = kvh * g + (row - n * g);
             uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
@@ -485,24 +508,20 @@ __device__ __forceinline__ f32x16 at_mfma6(const bf16x8 (&a)[3], const bf16x8 (&
 // matrix instructions a product: 419 TFLOP/s at most instead of the fp32
 // instruction's 157.  K and V are split once a tile, on their way to LDS (the
 // next tile's rows wait in registers); Q once, the weights where they form.
-// Waves: four with 32 rows of their own; or, sharing 32 rows (KS), four, or
-// two above 64 channels, where the parts of more sources would not fit LDS.
-template <int DB, bool KS>
+// Four waves with 32 rows of their own.
+template <int DB>
 struct AtF32 {
-    static constexpr int kWaves = KS && DB > 2 ? 2 : 4;
-    static constexpr int KT = KS ? 32 * kWaves : DB > 2 ? 32 : 64;      // sources of a tile
-    static constexpr int NB = KS ? 1 : KT / 32;
+    static constexpr int KT = DB > 2 ? 32 : 64;                         // sources of a tile
     static constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;           // 16-byte chunks of a row of one part
     static constexpr int kPart = KT * CH * 16;                          // bytes of one part of a tile
-    static constexpr int kUnits = KT * CH / (64 * kWaves);              // chunks of K (and of V) a thread stages
-    static constexpr int kJoin = KS ? kWaves * (32 * DB * 32 + 2 * 32) * 4 : 0;
-    static constexpr int kLds = 6 * kPart > kJoin ? 6 * kPart : kJoin;
+    static constexpr int kUnits = KT * CH / kAtThreads;                 // chunks of K (and of V) a thread stages
+    static constexpr int kLds = 6 * kPart;
 };
 
-template <int DB, bool KS, bool GEN>
-__global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) void attention_f32_kernel(AttnArgs a) {
-    using P = AtF32<DB, KS>;
-    constexpr int CH = P::CH, KT = P::KT, NB = P::NB, kThreads = 64 * P::kWaves;
+template <int DB, bool GEN>
+__global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_kernel(AttnArgs a) {
+    using P = AtF32<DB>;
+    constexpr int CH = P::CH, KT = P::KT, NB = KT / 32;
     extern __shared__ __align__(16) char lds[];              // K's three parts, then V's
 
     const int64_t lb = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
@@ -548,7 +567,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
     };
 
     // the wave's queries: operand B, channel 16 s + 8 half + e
-    const int row = tile0 * (KS ? 32 : 128) + (KS ? 0 : wave * 32) + col;
+    const int row = tile0 * 128 + wave * 32 + col;
     bf16x8 qf[2 * DB][3];
     {
         const int r = min(row, a.rows - 1), n = r / g, h = kvh * g + (r - n * g);
@@ -566,21 +585,19 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         }
     }
 
-    auto valid_bits = [&](int t, uint64_t (&bits)[(KT + 63) / 64]) {
-#pragma unroll
-        for (int i = 0; i < (KT + 63) / 64; ++i) {
-            const int64_t j = begin + (int64_t)t * KT + 64 * i;
-            bits[i] = at_count_bits(j, end);
-            if (mask) bits[i] &= ballot(j + lane < end && mask[j + lane]);
-        }
+    auto valid_bits = [&](int t) {
+        const int64_t j = begin + (int64_t)t * KT;
+        uint64_t bits = at_count_bits(j, end);
+        if (mask) bits &= ballot(j + lane < end && mask[j + lane]);
+        return bits;
     };
     float kr[P::kUnits][8], vr[P::kUnits][8];
-    auto fetch = [&](int t, const uint64_t (&bits)[(KT + 63) / 64]) {
+    auto fetch = [&](int t, uint64_t bits) {
         const int64_t j0 = begin + (int64_t)t * KT;
 #pragma unroll
         for (int i = 0; i < P::kUnits; ++i) {
-            const int p = i * kThreads + tid, r = p / CH, ch = (p % CH) ^ at_swz<CH>(r);
-            const bool ok = (bits[KT > 64 ? r >> 6 : 0] >> (r & 63)) & 1;
+            const int p = i * kAtThreads + tid, r = p / CH, ch = (p % CH) ^ at_swz<CH>(r);
+            const bool ok = (bits >> r) & 1;
             read8(kp + (j0 + r) * a.kl, 8 * ch, ok, kr[i]);
             read8(vp + (j0 + r) * a.vl, 8 * ch, ok, vr[i]);
         }
@@ -591,7 +608,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
             uint4 w[3], x[3];
             at_split8(kr[i], w);
             at_split8(vr[i], x);
-            char* d = lds + (i * kThreads + tid) * 16;
+            char* d = lds + (i * kAtThreads + tid) * 16;
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
                 *reinterpret_cast<uint4*>(d + k * P::kPart) = w[k];
@@ -612,9 +629,9 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
     const int vrow = 4 * half + (vi >> 2);
     const int vch = 2 * vg + ((vi & 3) >> 1), vin = 8 * (vi & 1);
 
-    uint64_t cur[(KT + 63) / 64], nxt[(KT + 63) / 64] = {};
+    uint64_t cur = 0, nxt = 0;
     if (tiles > 0) {
-        valid_bits(0, cur);
+        cur = valid_bits(0);
         fetch(0, cur);
     }
     for (int t = 0; t < tiles; ++t) {
@@ -622,7 +639,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         store();
         __syncthreads();
         if (t + 1 < tiles) {
-            valid_bits(t + 1, nxt);
+            nxt = valid_bits(t + 1);
             fetch(t + 1, nxt);
         }
         const char* tk = lds;
@@ -631,7 +648,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         f32x16 s[NB];
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
-            const char* base = tk + (32 * (KS ? wave : kb) + col) * CH * 16;
+            const char* base = tk + (32 * kb + col) * CH * 16;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.0f;
             bf16x8 kf[2][3];
@@ -650,8 +667,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         }
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
-            const int blk = KS ? wave : kb;
-            const uint32_t w32 = (uint32_t)(cur[KT > 64 ? blk >> 1 : 0] >> (32 * (blk & 1)));
+            const uint32_t w32 = (uint32_t)(cur >> (32 * kb));
             if (w32 != 0xffffffffu) {
                 const uint32_t w = w32 >> (4 * half);
 #pragma unroll
@@ -679,7 +695,6 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
-            const int blk = KS ? wave : kb;
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
                 // this step's 16 weights, sources 16 st + 8 (e / 4) + 4 half + e % 4
@@ -701,7 +716,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
                         s16x4 v[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const int vr0 = 32 * blk + 16 * st + 8 * e + vrow;
+                            const int vr0 = 32 * kb + 16 * st + 8 * e + vrow;
                             const int ch = (4 * d + vch) ^ (at_swz<CH>(vrow) | 2 * e);
                             v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                 (lds_s16x4)(tv + i * P::kPart + vr0 * CH * 16 + (ch << 4) + vin));
@@ -715,8 +730,7 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
                 }
             }
         }
-#pragma unroll
-        for (int i = 0; i < (KT + 63) / 64; ++i) cur[i] = nxt[i];
+        cur = nxt;
     }
 
     {
@@ -724,42 +738,183 @@ __global__ __launch_bounds__((64 * AtF32<DB, KS>::kWaves), (DB > 2 ? 1 : 2)) voi
         const float hi = at_other_half(l, lo);
         l = lo + hi;
     }
-    if constexpr (KS) {
-        constexpr int Dp = 32 * DB, W = P::kWaves;
-        float* sh = reinterpret_cast<float*>(lds);
-        float* sm = sh + W * Dp * 32;
-        __syncthreads();
+    if (row >= a.rows) return;
+    if (a.splits > 1) {
+        at_write_part<DB>(a, (pair * a.splits + split) * a.rows + row, oacc, m, l, half);
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int n = row / g, h = kvh * g + (row - n * g);
+    float* op = static_cast<float*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                sh[(wave * Dp + 32 * d + 8 * (r / 4) + 4 * half + r % 4) * 32 + col] = oacc[d][r];
-        if (half == 0) {
-            sm[wave * 32 + col] = m;
-            sm[(W + wave) * 32 + col] = l;
+        for (int r = 0; r < 16; r += 4) {
+            const int d0 = 32 * d + 2 * r + 4 * half;
+            if constexpr (GEN) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d0 + e < a.D) op[d0 + e] = oacc[d][r + e] * inv;
+            } else if (d0 < a.D) {
+                *reinterpret_cast<float4*>(op + d0) = make_float4(oacc[d][r] * inv, oacc[d][r + 1] * inv,
+                                                                  oacc[d][r + 2] * inv, oacc[d][r + 3] * inv);
+            }
         }
-        __syncthreads();
-        at_join_waves<float, Dp, W>(a, sh, sm, tile0 * 32, pair, split, b, kvh, g);
-    } else {
-        if (row >= a.rows) return;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int n = row / g, h = kvh * g + (row - n * g);
-        float* op = static_cast<float*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+}
+
+// Few rows in fp32: 16 RB query rows, the fp32 instruction, and K and V from
+// memory straight to its operands, so that nothing waits for a tile: the
+// waves take blocks of 16 sources in turn and join at the end.  On
+// v_mfma_f32_16x16x4_f32 a lane supplies row or column lane % 16 and one k, lane
+// / 16 = g.  Scores: the k of a step are channels 16 i + 4 g + e, so that a
+// lane's 16 bytes of its source's row are four steps; a lane's four scores are
+// sources 4 g + r of query lane % 16.  Outputs: step r takes source 4 g + r,
+// and 16 bytes of its row, channels 64 q + 4 (lane % 16) + e, are four blocks'
+// operands.
+// Bound: one read of K and V (157 TFLOP/s hold 20 bytes a clock and compute
+// unit for 16 rows).
+template <int DQ, int RB, bool GEN>
+__global__ __launch_bounds__(kAtThreads, (DQ * RB > 2 ? 1 : 2)) void attention_f32_few_kernel(AttnArgs a) {
+    constexpr int R = 16 * RB, W = kAtThreads / 64;
+    extern __shared__ __align__(16) char lds[];              // the waves' sums, then their maxima and sums of weights
+    float* sh = reinterpret_cast<float*>(lds);
+    float* sm = sh + W * 64 * DQ * R;
+    const int64_t lb = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (lb >= a.blocks) return;
+    const int split = (int)(lb % a.splits);
+    const int64_t rest = lb / a.splits;
+    const int tile0 = (int)(rest % a.row_tiles);
+    const int64_t pair = rest / a.row_tiles;
+    const int64_t b = pair / a.Hkv;
+    const int kvh = (int)(pair - b * a.Hkv), g = a.Hq / a.Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int l16 = lane & 15, grp = lane >> 4;
+
+    const float* __restrict__ kp = static_cast<const float*>(a.k) + b * a.kb + kvh * a.kh;
+    const float* __restrict__ vp = static_cast<const float*>(a.v) + b * a.vb + kvh * a.vh;
+    const uint8_t* __restrict__ mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
+    int64_t end = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
+    int64_t begin = 0;
+    if (a.splits > 1) {
+        const int64_t per = ((end + a.splits - 1) / a.splits + 63) / 64 * 64;
+        begin = min(end, split * per);
+        end = min(end, begin + per);
+    }
+    const float c0 = a.scale * 1.44269504088896340736f;
+    const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
+    auto read4 = [&](const float* p, int d0, bool ok) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (GEN) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+            for (int e = 0; e < 4; ++e)
+                if (ok && d0 + e < a.D) v[e] = p[d0 + e];
+        } else {                     // D is a multiple of 4
+            if (ok && d0 < a.D) v = *reinterpret_cast<const f32x4*>(p + d0);
+        }
+        return v;
+    };
+    f32x4 qf[RB][4 * DQ];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d0 = 32 * d + 2 * r + 4 * half;
-                if constexpr (GEN) {
+    for (int j = 0; j < RB; ++j) {
+        const int r = min(tile0 * R + 16 * j + l16, a.rows - 1), n = r / g, h = kvh * g + (r - n * g);
+        const float* qp = static_cast<const float*>(a.q) + b * a.qb + n * a.ql + h * a.qh;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (d0 + e < a.D) op[d0 + e] = oacc[d][r + e] * inv;
-                } else if (d0 < a.D) {
-                    *reinterpret_cast<float4*>(op + d0) = make_float4(oacc[d][r] * inv, oacc[d][r + 1] * inv,
-                                                                      oacc[d][r + 2] * inv, oacc[d][r + 3] * inv);
+        for (int i = 0; i < 4 * DQ; ++i) {
+            qf[j][i] = read4(qp, 16 * i + 4 * grp, true);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qf[j][i][e] = c0 == 0.0f ? 0.0f : c0 < 0.0f ? -qf[j][i][e] : qf[j][i][e];
+        }
+    }
+    f32x4 o[RB][DQ][4];
+    float m[RB], l[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        m[j] = -INFINITY;
+        l[j] = 0.0f;
+#pragma unroll
+        for (int q = 0; q < DQ; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[j][q][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int64_t j0 = begin + 16 * wave; j0 < end; j0 += 16 * W) {
+        const bool ok = j0 + l16 < end && (!mask || mask[j0 + l16]);
+        const uint32_t bits = (uint32_t)ballot(ok) & 0xffffu;
+        f32x4 kf[4 * DQ], vf[4][DQ];
+#pragma unroll
+        for (int i = 0; i < 4 * DQ; ++i) kf[i] = read4(kp + (j0 + l16) * a.kl, 16 * i + 4 * grp, ok);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int q = 0; q < DQ; ++q)
+                vf[r][q] = read4(vp + (j0 + 4 * grp + r) * a.vl, 64 * q + 4 * l16, (bits >> (4 * grp + r)) & 1);
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+#pragma unroll
+            for (int i = 0; i < 4 * DQ; ++i) {
+                if (16 * i >= a.D) break;
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][e], qf[j][i][e], s0, 0, 0, 0);
+                    s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][e + 1], qf[j][i][e + 1], s1, 0, 0, 0);
                 }
             }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s0[r] = (bits >> (4 * grp + r)) & 1 ? s0[r] + s1[r] : -INFINITY;
+                mx = fmaxf(mx, s0[r]);
+            }
+            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            float lo;
+            const float hi = at_other_half(mx, lo);
+            mx = fmaxf(lo, hi) * c;
+            if (ballot(mx > m[j] + 8.0f)) {
+                const float mn = fmaxf(m[j], mx);
+                const float f = mn == -INFINITY ? 1.0f : at_exp2(m[j] - mn);
+                m[j] = mn;
+                l[j] *= f;
+#pragma unroll
+                for (int q = 0; q < DQ; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[j][q][e] *= f;
+            }
+            const float base = m[j] == -INFINITY ? 0.0f : m[j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = at_exp2(fmaf(s0[r], c, -base));
+                l[j] += p;
+#pragma unroll
+                for (int q = 0; q < DQ; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[j][q][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[r][q][e], p, o[j][q][e], 0, 0, 0);
+            }
+        }
     }
+    // a query's four lanes join their sums, then the waves
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[j]), __float_as_uint(l[j]), false, false);
+        l[j] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+        float lo;
+        const float hi = at_other_half(l[j], lo);
+        l[j] = lo + hi;
+#pragma unroll
+        for (int q = 0; q < DQ; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sh[(wave * 64 * DQ + 64 * q + 16 * grp + 4 * r + e) * R + 16 * j + l16] = o[j][q][e][r];
+        if (grp == 0) {
+            sm[wave * R + 16 * j + l16] = m[j];
+            sm[(W + wave) * R + 16 * j + l16] = l[j];
+        }
+    }
+    __syncthreads();
+    at_join_waves<float, 64 * DQ, W, R>(a, sh, sm, tile0 * R, pair, split, b, kvh, g);
 }
 
 constexpr int kAtMaxSplits = 256;
@@ -767,14 +922,14 @@ constexpr int kAtMaxSplits = 256;
 // The splits' results of one row, joined: their weights first, a split per
 // thread, then the sums, 32 lanes of 4 channels over every eighth split.
 template <typename T>
-__global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, int Dp) {
+__global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a) {
     __shared__ float w[kAtMaxSplits], red[4];
     __shared__ float4 sum[kAtThreads / 32][32];
     const int tid = threadIdx.x, lane = tid & 31, grp = tid >> 5;
     const int64_t pair = blockIdx.x / a.rows;
     const int row = (int)(blockIdx.x - pair * a.rows);
     const int64_t first = pair * a.splits * a.rows + row;
-    const float* pm = a.part + (int64_t)gridDim.x * a.splits * Dp;
+    const float* pm = a.part + (int64_t)gridDim.x * a.splits * a.Dp;
     float m = -INFINITY, l = 0.0f;
     if (tid < a.splits) {
         const float2 v = *reinterpret_cast<const float2*>(pm + 2 * (first + tid * (int64_t)a.rows));
@@ -800,7 +955,7 @@ __global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, 
         for (int s = grp; s < a.splits; s += kAtThreads / 32) {
             const float fs = w[s];
             if (fs == 0.0f) continue;
-            const float4 x = *reinterpret_cast<const float4*>(a.part + (first + s * (int64_t)a.rows) * Dp + 4 * lane);
+            const float4 x = *reinterpret_cast<const float4*>(a.part + (first + s * (int64_t)a.rows) * a.Dp + 4 * lane);
             v.x += fs * x.x; v.y += fs * x.y; v.z += fs * x.z; v.w += fs * x.w;
         }
     }
@@ -824,7 +979,7 @@ __global__ __launch_bounds__(kAtThreads) void attention_join_kernel(AttnArgs a, 
 // How a call is split: QB blocks of query rows per wave, or the waves sharing
 // 32 rows (qb = 0), and `splits` workgroups over the sources.
 struct AttnPlan {
-    int qb, row_tiles, splits, Dp;
+    int qb, rb, row_tiles, splits, Dp;      // rb: blocks of 16 shared rows of the fp32 form
     int64_t blocks;
 };
 
@@ -833,17 +988,32 @@ constexpr int kAtCus = 256;
 AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int D, int dtype) {
     AttnPlan p;
     const int64_t pairs = B * Hkv, rows = Nq * (Hq / Hkv);
+    const int64_t wg1 = pairs * ceil_div(rows, 128);
     p.Dp = (D + 31) / 32 * 32;
     p.splits = 1;
+    p.rb = 0;
+    auto splits = [&](int64_t wg) {
+        return (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 256)));
+    };
+    // Two blocks a wave read the sources' operands half as often (64 channels: 585 -> 564 us for 4 x 16384 over 4096, 8
+    // heads) but above 64 channels leave one wave a SIMD (128: 1080 -> 1260 us).  Below a workgroup for most compute
+    // units, waves that share 32 rows and split the sources finish sooner (1 x 1024 over 1024, 8 heads of 64: 11 us
+    // instead of 22); in fp32, whose shared form is the slower instruction, only for few rows (4 x 349 over 10357, 4
+    // heads on 2, of 24: 79 us with rows of their own, 235 shared).
     if (dtype == MESORASI_BF16 && D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
         p.qb = 2;
-    else if (pairs * ceil_div(rows, 128) >= kAtCus * 3 / 4)
+    else if (wg1 >= kAtCus * 3 / 4 || (dtype == MESORASI_F32 && rows > 64))
         p.qb = 1;
     else
         p.qb = 0;
-    p.row_tiles = (int)ceil_div(rows, p.qb ? 128 * p.qb : 32);
+    int tile = 128 * p.qb;
+    if (p.qb == 0) {
+        if (dtype == MESORASI_F32) p.rb = rows <= 16 ? 1 : 2;
+        tile = p.rb == 1 ? 16 : 32;
+    }
+    p.row_tiles = (int)ceil_div(rows, tile);
     const int64_t wg = pairs * p.row_tiles;
-    if (p.qb == 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 256)));
+    if (p.qb < 2) p.splits = splits(wg);
     p.blocks = wg * p.splits;
     return p;
 }
@@ -885,28 +1055,41 @@ int launch_attention_bf16(const AttnArgs& a, int qb, unsigned grid, hipStream_t 
     }
 }
 
-template <int DB, bool KS, bool GEN>
+template <int DB, bool GEN>
 int launch_attention_f32(const AttnArgs& a, unsigned grid, hipStream_t s) {
-    using P = AtF32<DB, KS>;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_f32_kernel<DB, KS, GEN>),
+    using P = AtF32<DB>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_f32_kernel<DB, GEN>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, P::kLds);
     MESO_REQUIRE(attr == hipSuccess, MESORASI_EHIP, "mesorasi_cross_attention: LDS size attribute: %s",
                  hipGetErrorString(attr));
-    attention_f32_kernel<DB, KS, GEN><<<dim3(grid), dim3(64 * P::kWaves), P::kLds, s>>>(a);
+    attention_f32_kernel<DB, GEN><<<dim3(grid), dim3(kAtThreads), P::kLds, s>>>(a);
+    return MESORASI_OK;
+}
+
+template <int DQ, int RB, bool GEN>
+int launch_attention_f32_few(const AttnArgs& a, unsigned grid, hipStream_t s) {
+    constexpr int bytes = kAtThreads / 64 * (64 * DQ + 2) * 16 * RB * 4;
+    static const hipError_t attr =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_f32_few_kernel<DQ, RB, GEN>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    MESO_REQUIRE(attr == hipSuccess, MESORASI_EHIP, "mesorasi_cross_attention: LDS size attribute: %s",
+                 hipGetErrorString(attr));
+    attention_f32_few_kernel<DQ, RB, GEN><<<dim3(grid), dim3(kAtThreads), bytes, s>>>(a);
     return MESORASI_OK;
 }
 
 template <bool GEN>
-int launch_attention_f32(const AttnArgs& a, int qb, unsigned grid, hipStream_t s) {
-    switch ((a.D + 31) / 32 * 2 + (qb == 0)) {
-        case 2: return launch_attention_f32<1, false, GEN>(a, grid, s);
-        case 3: return launch_attention_f32<1, true, GEN>(a, grid, s);
-        case 4: return launch_attention_f32<2, false, GEN>(a, grid, s);
-        case 5: return launch_attention_f32<2, true, GEN>(a, grid, s);
-        case 6: return launch_attention_f32<3, false, GEN>(a, grid, s);
-        case 7: return launch_attention_f32<3, true, GEN>(a, grid, s);
-        case 8: return launch_attention_f32<4, false, GEN>(a, grid, s);
-        default: return launch_attention_f32<4, true, GEN>(a, grid, s);
+int launch_attention_f32(const AttnArgs& a, const AttnPlan& p, unsigned grid, hipStream_t s) {
+    if (p.qb == 0) {
+        if (a.D <= 64)
+            return p.rb == 1 ? launch_attention_f32_few<1, 1, GEN>(a, grid, s) : launch_attention_f32_few<1, 2, GEN>(a, grid, s);
+        return p.rb == 1 ? launch_attention_f32_few<2, 1, GEN>(a, grid, s) : launch_attention_f32_few<2, 2, GEN>(a, grid, s);
+    }
+    switch ((a.D + 31) / 32) {
+        case 1: return launch_attention_f32<1, GEN>(a, grid, s);
+        case 2: return launch_attention_f32<2, GEN>(a, grid, s);
+        case 3: return launch_attention_f32<3, GEN>(a, grid, s);
+        default: return launch_attention_f32<4, GEN>(a, grid, s);
     }
 }
 
@@ -962,6 +1145,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     a.row_tiles = p.row_tiles;
     a.splits = p.splits;
     a.blocks = p.blocks;
+    a.Dp = p.Dp;
     a.part = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
     const int64_t per = ceil_div(p.blocks, 8);
     MESO_REQUIRE(per <= 0x7fffffff / 8, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
@@ -973,16 +1157,16 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     const bool vec = st % (f32 ? 4 : 8) == 0 && (o_bs | o_ld | o_hs) % 4 == 0 && aligned(q, 16) && aligned(k, 16) &&
                      aligned(v, 16) && aligned(o, f32 ? 16 : 8);
     const unsigned grid = (unsigned)(8 * per);
-    const int rc = f32 ? (vec ? launch_attention_f32<false>(a, p.qb, grid, s) : launch_attention_f32<true>(a, p.qb, grid, s))
+    const int rc = f32 ? (vec ? launch_attention_f32<false>(a, p, grid, s) : launch_attention_f32<true>(a, p, grid, s))
                        : (vec ? launch_attention_bf16<false>(a, p.qb, grid, s)
                               : launch_attention_bf16<true>(a, p.qb, grid, s));
     if (rc != MESORASI_OK) return rc;
     if (p.splits > 1) {
         const dim3 jgrid((unsigned)(pairs * a.rows)), block(kAtThreads);
         if (f32)
-            attention_join_kernel<float><<<jgrid, block, 0, s>>>(a, p.Dp);
+            attention_join_kernel<float><<<jgrid, block, 0, s>>>(a);
         else
-            attention_join_kernel<uint16_t><<<jgrid, block, 0, s>>>(a, p.Dp);
+            attention_join_kernel<uint16_t><<<jgrid, block, 0, s>>>(a);
     }
     return after_launch("mesorasi_cross_attention");
 }

@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kGnThreads = 256;      // of the two-launch form
 constexpr int kGnOneThreads = 512;   // of the one-launch form
-constexpr int kGnKeep = 16;          // vectors of a thread in the one-launch form
+constexpr int kGnKeep = 16;          // vectors of a thread in the one-launch form, at most
 constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit
 
 template <typename T, int N>
@@ -424,7 +424,7 @@ __device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int n
 
 // One launch: the slab's valid rows stay in registers between the
 // statistics and the output, so the variance is taken about the mean.
-template <typename TX, typename TY, int VEC, int ACT>
+template <typename TX, typename TY, int VEC, int ACT, int KEEP>
 __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     __shared__ float ent[kGnOneThreads * VEC];   // [slots][width], at most a value for each thread and channel
     __shared__ float sums[kGnOneThreads * VEC];  // a slab's groups: at most its channels
@@ -441,16 +441,16 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     TY* __restrict__ yp = static_cast<TY*>(a.y) + (p.b * a.N + p.slot) * a.ldy + p.ch0 + p.vec * VEC;
     GnChannels<VEC> c;
     gn_channels<TX, VEC, true>(a, p, c);
-    GnVec<TX, VEC> w[kGnKeep];
+    GnVec<TX, VEC> w[KEEP];
 #pragma unroll
-    for (int i = 0; i < kGnKeep; ++i)
+    for (int i = 0; i < KEEP; ++i)
         if (i < mine) w[i] = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + (int64_t)i * p.slots * a.ldx);
     float A[VEC] = {}, S[VEC] = {};
     if (nrows > 0) {
         const float inv = 1.0f / ((float)nrows * (float)a.c);
         float v[VEC] = {}, mean[VEC];
 #pragma unroll
-        for (int i = 0; i < kGnKeep; ++i)
+        for (int i = 0; i < KEEP; ++i)
             if (i < mine)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) v[k] += gn_float(w[i].e[k]) - c.ref[k];
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
             v[k] = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < kGnKeep; ++i)
+        for (int i = 0; i < KEEP; ++i)
             if (i < mine)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     }
     if (!p.on) return;
 #pragma unroll
-    for (int i = 0; i < kGnKeep; ++i)
+    for (int i = 0; i < KEEP; ++i)
         if (i < mine) {
             GnVec<TY, VEC> o;
 #pragma unroll
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
 
 // How a call is cut.
 struct GnPlan {
-    bool one;
+    int keep;            // one launch, with this many vectors a thread; 0: two launches
     int slab, slabs, pieces, chunks;
     int64_t chunk_rows;
 };
@@ -507,13 +507,16 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
     // the shortest run of whole groups and whole vectors (C is a multiple of both)
     const int64_t base = (int64_t)c / gn_gcd(c, vec) * vec;
     const int64_t room = (int64_t)kGnOneThreads * kGnKeep;
-    auto fits = [&](int64_t slab) {
-        int64_t nvp = 1;               // lanes of a row, a power of two
-        while (nvp < slab / vec) nvp *= 2;
-        return nvp <= kGnOneThreads && ceil_div(N, kGnOneThreads / nvp) <= kGnKeep;
+    auto lanes = [&](int64_t slab) {         // of a row, a power of two
+        int64_t n = 1;
+        while (n < slab / vec) n *= 2;
+        return n;
     };
-    p.one = base <= C && N <= room && fits(base);
-    if (p.one) {
+    auto fits = [&](int64_t slab) {
+        return lanes(slab) <= kGnOneThreads && ceil_div(N, kGnOneThreads / lanes(slab)) <= kGnKeep;
+    };
+    p.keep = 0;
+    if (base <= C && N <= room && fits(base)) {
         // longer runs read whole lines; not past 256 bytes, nor below a workgroup for each compute unit
         int64_t slab = base;
         while (2 * slab <= C && C % (2 * slab) == 0 && 2 * slab / vec <= 16 && fits(2 * slab) &&
@@ -521,6 +524,7 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
             slab *= 2;
         p.slab = (int)slab;
         p.slabs = (int)(C / slab);
+        p.keep = ceil_div(N, kGnOneThreads / lanes(slab)) <= kGnKeep / 4 ? kGnKeep / 4 : kGnKeep;
         return p;
     }
     const int64_t most = (int64_t)kGnThreads * vec;
@@ -547,22 +551,26 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
 }
 
 size_t group_norm_ws(const GnPlan& p, int64_t B, int G) {
-    return p.one ? 0 : ((size_t)(B * p.chunks * G * p.pieces) * 8 + 15) / 16 * 16;
+    return p.keep ? 0 : ((size_t)(B * p.chunks * G * p.pieces) * 8 + 15) / 16 * 16;
 }
 
 // Widest vector: 16 bytes of x where C allows them, else single values.
 int group_norm_vec(int C, int G, int x_dtype) {
     const int vec = x_dtype == MESORASI_F32 ? 4 : 8;
-    const int c = C / G;
-    // whole vectors in a row, and in a group where it is cut into pieces
-    return C % vec == 0 && (c % vec == 0 || c <= 64) ? vec : 1;
+    const int64_t c = C / G;
+    // whole vectors in a row, and in a group, or in a run of groups within the threads' vectors
+    return C % vec == 0 && (c % vec == 0 || c / gn_gcd(c, vec) <= kGnThreads) ? vec : 1;
 }
 
 template <typename TX, typename TY, int VEC, int ACT>
 void launch_group_norm(const GnArgs& a, const GnPlan& p, hipStream_t s) {
     const int64_t blocks = a.B * a.slabs * a.chunks;
-    if (p.one) {
-        gn_one_kernel<TX, TY, VEC, ACT><<<dim3((unsigned)blocks), dim3(kGnOneThreads), 0, s>>>(a);
+    if (p.keep) {
+        const dim3 grid((unsigned)blocks), block(kGnOneThreads);
+        if (p.keep < kGnKeep)
+            gn_one_kernel<TX, TY, VEC, ACT, kGnKeep / 4><<<grid, block, 0, s>>>(a);
+        else
+            gn_one_kernel<TX, TY, VEC, ACT, kGnKeep><<<grid, block, 0, s>>>(a);
         return;
     }
     gn_parts_kernel<TX, VEC><<<dim3((unsigned)blocks), dim3(kGnThreads), 0, s>>>(a);

@@ -23,6 +23,12 @@ struct alignas(sizeof(T) * N) QuVec {
     T e[N];
 };
 
+// The same at any element: the hardware's loads need no more.
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) QuLoose {
+    T e[N];
+};
+
 __device__ __forceinline__ float qu_float(float v) { return v; }
 __device__ __forceinline__ float qu_float(uint16_t v) { return bf16_to_f32(v); }
 
@@ -50,39 +56,43 @@ __device__ __forceinline__ uint32_t qu_byte(float v, float inv) {
 
 template <int N>
 __device__ __forceinline__ void qu_store(int8_t* q, const float (&f)[N], const QuScale& s) {
-    if constexpr (N == 1) {
-        *q = s.bad ? 0 : (int8_t)qu_byte(f[0], s.inv);
-    } else {
-        QuVec<uint32_t, N / 4> w;
+    QuVec<uint32_t, N / 4> w;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            uint32_t u = 0;
+    for (int i = 0; i < N / 4; ++i) {
+        uint32_t u = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u |= qu_byte(f[4 * i + k], s.inv) << (8 * k);
-            w.e[i] = s.bad ? 0u : u;
-        }
-        *reinterpret_cast<QuVec<uint32_t, N / 4>*>(q) = w;
+        for (int k = 0; k < 4; ++k) u |= qu_byte(f[4 * i + k], s.inv) << (8 * k);
+        w.e[i] = s.bad ? 0u : u;
     }
+    *reinterpret_cast<QuVec<uint32_t, N / 4>*>(q) = w;
 }
 
-// LPR lanes per row, VEC columns at a time; the first kQuKeep vectors of a
-// lane stay in registers between the maximum and the rounding, longer rows
-// are read again.  Bound: one read of x and one write of q.
-template <typename T, int VEC, int LPR>
+// LPR lanes per row, 16 bytes of a row (of any alignment) at a time; the first
+// kQuKeep vectors of a lane stay in registers between the maximum and the
+// rounding, longer rows are read again.  Bound: one read of x and one write
+// of q.
+template <typename T, int LPR>
 __global__ __launch_bounds__(kQuThreads) void quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows,
                                                                  int C, int8_t* __restrict__ q, int64_t ldq,
                                                                  float* __restrict__ scale) {
+    constexpr int VEC = 16 / sizeof(T);
     const int64_t r = blockIdx.x * (int64_t)(kQuThreads / LPR) + threadIdx.x / LPR;
     const int lane = threadIdx.x % LPR;
     if (r >= rows) return;
     const T* xr = x + r * ldx;
-    const int nv = (C + VEC - 1) / VEC;              // VEC == 1 or C % VEC == 0
+    const int pad = (C + 15) & ~15, nv = pad / VEC;          // the last vectors may end in padding
     float keep[kQuKeep][VEC];
     uint32_t m = 0;
     auto read = [&](int v, float (&f)[VEC]) {
-        const QuVec<T, VEC> w = *reinterpret_cast<const QuVec<T, VEC>*>(xr + v * VEC);
+        const int c = v * VEC;
+        if (c + VEC <= C) {
+            const QuLoose<T, VEC> w = *reinterpret_cast<const QuLoose<T, VEC>*>(xr + c);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) f[i] = qu_float(w.e[i]);
+            for (int i = 0; i < VEC; ++i) f[i] = qu_float(w.e[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[i] = c + i < C ? qu_float(xr[c + i]) : 0.0f;
+        }
     };
 #pragma unroll
     for (int i = 0; i < kQuKeep; ++i) {
@@ -114,38 +124,27 @@ __global__ __launch_bounds__(kQuThreads) void quantize_i8_kernel(const T* __rest
         read(v, f);
         qu_store<VEC>(qr + v * VEC, f, s);
     }
-    for (int c = C + lane; c < ((C + 15) & ~15); c += LPR) qr[c] = 0;
 }
 
-template <typename T, int VEC>
-void launch_quantize(const T* x, int64_t ldx, int64_t rows, int C, int8_t* q, int64_t ldq, float* scale,
-                     hipStream_t s) {
-    const int nv = (C + VEC - 1) / VEC;
+template <typename T>
+void run_quantize(const T* x, int64_t ldx, int64_t rows, int C, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
+    const int nv = ((C + 15) & ~15) / (16 / (int)sizeof(T));
     // as few lanes as keep a row in registers, so that short rows share a wave
     const int lpr = nv <= 4 * kQuKeep ? 4 : nv <= 16 * kQuKeep ? 16 : 64;
     const dim3 grid((unsigned)ceil_div(rows, kQuThreads / lpr)), block(kQuThreads);
     switch (lpr) {
-        case 4: quantize_i8_kernel<T, VEC, 4><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
-        case 16: quantize_i8_kernel<T, VEC, 16><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
-        default: quantize_i8_kernel<T, VEC, 64><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
+        case 4: quantize_i8_kernel<T, 4><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
+        case 16: quantize_i8_kernel<T, 16><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
+        default: quantize_i8_kernel<T, 64><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
     }
 }
 
 void run_quantize(const void* x, int64_t ldx, int dtype, int64_t rows, int C, int8_t* q, int64_t ldq, float* scale,
                   hipStream_t s) {
-    if (dtype == MESORASI_F32) {
-        const float* p = static_cast<const float*>(x);
-        if (C % 4 == 0 && ldx % 4 == 0 && aligned(p, 16))
-            launch_quantize<float, 4>(p, ldx, rows, C, q, ldq, scale, s);
-        else
-            launch_quantize<float, 1>(p, ldx, rows, C, q, ldq, scale, s);
-    } else {
-        const uint16_t* p = static_cast<const uint16_t*>(x);
-        if (C % 8 == 0 && ldx % 8 == 0 && aligned(p, 16))
-            launch_quantize<uint16_t, 8>(p, ldx, rows, C, q, ldq, scale, s);
-        else
-            launch_quantize<uint16_t, 1>(p, ldx, rows, C, q, ldq, scale, s);
-    }
+    if (dtype == MESORASI_F32)
+        run_quantize(static_cast<const float*>(x), ldx, rows, C, q, ldq, scale, s);
+    else
+        run_quantize(static_cast<const uint16_t*>(x), ldx, rows, C, q, ldq, scale, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -364,8 +363,7 @@ constexpr int kFewSteps = 4;         // steps of 64 columns that a wave holds in
 constexpr int kFewMaxK = 64 * 8 * kFewSteps;
 
 template <typename TX, typename TY, int RB>
-__global__ __launch_bounds__(kFewThreads) void linear_i8_few_kernel(LinArgs a, const TX* __restrict__ xf, int ci,
-                                                                    int vec_x) {
+__global__ __launch_bounds__(kFewThreads) void linear_i8_few_kernel(LinArgs a, const TX* __restrict__ xf, int ci) {
     constexpr int kWaves = kFewThreads / 64;
     __shared__ i32x4 part[kWaves][RB][64];
     __shared__ uint32_t top[kWaves][16];
@@ -414,9 +412,9 @@ __global__ __launch_bounds__(kFewThreads) void linear_i8_few_kernel(LinArgs a, c
             constexpr int V = 16 / sizeof(TX);
 #pragma unroll
             for (int e = 0; e < 16; e += V) {
-                if (vec_x) {          // ci is a multiple of V
-                    QuVec<TX, V> w = {};
-                    if (row && k0 + e < ci) w = *reinterpret_cast<const QuVec<TX, V>*>(xp + 64 * (s0 + i) + e);
+                if (k0 + e + V <= ci) {
+                    QuLoose<TX, V> w = {};
+                    if (row) w = *reinterpret_cast<const QuLoose<TX, V>*>(xp + 64 * (s0 + i) + e);
 #pragma unroll
                     for (int k = 0; k < V; ++k) v[i][e + k] = qu_float(w.e[k]);
                 } else {
@@ -477,15 +475,17 @@ int run_linear(LinArgs& a, hipStream_t s) {
     if (a.rows <= 64) {
         const dim3 grid((unsigned)ceil_div(a.co, 16)), block(kFewThreads);
         if (a.rows <= 16)
-            linear_i8_few_kernel<int8_t, TY, 1><<<grid, block, 0, s>>>(a, nullptr, 0, 0);
+            linear_i8_few_kernel<int8_t, TY, 1><<<grid, block, 0, s>>>(a, nullptr, 0);
         else if (a.rows <= 32)
-            linear_i8_few_kernel<int8_t, TY, 2><<<grid, block, 0, s>>>(a, nullptr, 0, 0);
+            linear_i8_few_kernel<int8_t, TY, 2><<<grid, block, 0, s>>>(a, nullptr, 0);
         else
-            linear_i8_few_kernel<int8_t, TY, 4><<<grid, block, 0, s>>>(a, nullptr, 0, 0);
+            linear_i8_few_kernel<int8_t, TY, 4><<<grid, block, 0, s>>>(a, nullptr, 0);
         return MESORASI_OK;
     }
-    // 256 x 256 tiles for many long products, else the largest tile that gives most compute units one
-    if (a.kp >= 512 && ceil_div(a.rows, 256) * ceil_div(a.co, 256) >= 192) return launch_linear<TY, 2, 4, 4, 2>(a, s);
+    // 256 x 256 tiles for many long products, else the largest tile that gives most compute units one: 16384 x 1024 ->
+    // 1024 takes 32.5 us in the first and 34.6 in the second, 16384 x 320 -> 256 9.2 in the second and 8.6 in the third,
+    // 65536 x 128 -> 128 17.0, 11.9 and 11.9, 4096 x 1024 -> 1024 27.5, 11.3 and 12.3
+    if (a.kp >= 1024 && ceil_div(a.rows, 256) * ceil_div(a.co, 256) >= 192) return launch_linear<TY, 2, 4, 4, 2>(a, s);
     if (ceil_div(a.rows, 128) * ceil_div(a.co, 128) >= 192) return launch_linear<TY, 2, 4, 2, 1>(a, s);
     return launch_linear<TY, 2, 2, 1, 1>(a, s);
 }
@@ -497,10 +497,7 @@ bool linear_few_fused(int64_t rows, int64_t kp, int x_dtype) {
 
 template <typename TX, typename TY>
 void run_linear_few_fused(const LinArgs& a, const TX* x, int ci, hipStream_t s) {
-    constexpr int V = 16 / sizeof(TX);
-    const int vec_x = ci % V == 0 && a.ldx % V == 0 && aligned(x, 16);
-    linear_i8_few_kernel<TX, TY, 1>
-        <<<dim3((unsigned)ceil_div(a.co, 16)), dim3(kFewThreads), 0, s>>>(a, x, ci, vec_x);
+    linear_i8_few_kernel<TX, TY, 1><<<dim3((unsigned)ceil_div(a.co, 16)), dim3(kFewThreads), 0, s>>>(a, x, ci);
 }
 
 int64_t i8_pad(int64_t c) { return (c + 15) & ~(int64_t)15; }
