@@ -205,14 +205,22 @@ __device__ __forceinline__ void gn_channels(const GnArgs& a, const P& p, GnChann
     const TX* x0 = static_cast<const TX*>(a.x) + p.b * a.N * a.ldx + (int64_t)p.first * a.c;
     p.channel_groups(a, c.grp);
     const int ch = p.ch0 + p.vec * VEC;
+    const bool any = p.on && p.len > 0;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-        c.ref[k] = p.on && p.len > 0 ? gn_float(x0[c.grp[k] * a.c]) : 0.0f;
-        if (AFFINE) {
-            c.gamma[k] = p.on && a.gamma ? a.gamma[ch + k] : 1.0f;
-            c.beta[k] = p.on && a.beta ? a.beta[ch + k] : 0.0f;
-        }
+        c.ref[k] = 0.0f;
+        c.gamma[k] = 1.0f;
+        c.beta[k] = 0.0f;
     }
+    if (any)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) c.ref[k] = gn_float(x0[c.grp[k] * a.c]);
+    if (AFFINE && any && a.gamma)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) c.gamma[k] = a.gamma[ch + k];
+    if (AFFINE && any && a.beta)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) c.beta[k] = a.beta[ch + k];
 }
 
 // The thread's channels' parts (mean relative to its group's first value,
@@ -390,13 +398,13 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     for (; r < r1; r += p.slots) gn_store(yp + r * a.ldy, GnVec<TY, VEC>{});
 }
 
-// Sums over the workgroup of each group's values: a thread's per channel,
-// then over the rows of its wave, then over waves and channels.  A wave holds
+// Sums over the workgroup of each group's values, finished once a group: a
+// thread's per channel, then over the rows of its wave, then over waves and channels.  A wave holds
 // whole copies of the vectors' lanes (nvp of them, a power of two) or the
 // workgroup holds rows of several waves.
-template <int VEC, typename P>
+template <int VEC, typename P, typename Finish>
 __device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int nvp, float (&v)[VEC], float* ent,
-                                              float* res) {
+                                              float* res, Finish finish) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) v[k] = wave_sum_from(v[k], nvp);
@@ -417,7 +425,7 @@ __device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int n
         for (int s = s0; s < slots; s += ws)
             for (int e = e0; e < a.c; e += we) sum += ent[s * p.width + g * a.c + e];
         sum = lane_sum(sum, w);
-        if (l == 0) res[g] = sum;
+        if (l == 0) res[g] = finish(sum);
     }
     __syncthreads();
 }
@@ -454,10 +462,10 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
             if (i < mine)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) v[k] += gn_float(w[i].e[k]) - c.ref[k];
-        gn_group_sums<VEC>(a, p, nvp, v, ent, sums);
+        gn_group_sums<VEC>(a, p, nvp, v, ent, sums, [&](float sum) { return sum * inv; });
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-            mean[k] = sums[c.grp[k]] * inv;
+            mean[k] = sums[c.grp[k]];
             v[k] = 0.0f;
         }
 #pragma unroll
@@ -468,12 +476,9 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
                     const float d = (gn_float(w[i].e[k]) - c.ref[k]) - mean[k];
                     v[k] = fmaf(d, d, v[k]);
                 }
-        gn_group_sums<VEC>(a, p, nvp, v, ent, sums);
+        gn_group_sums<VEC>(a, p, nvp, v, ent, sums, [&](float sum) { return 1.0f / sqrtf(sum * inv + a.eps); });
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            if (mine > 0)
-                gn_factor(make_float2(mean[k], 1.0f / sqrtf(sums[c.grp[k]] * inv + a.eps)), c.gamma[k], c.beta[k], A[k],
-                          S[k]);
+        for (int k = 0; k < VEC; ++k) gn_factor(make_float2(mean[k], sums[c.grp[k]]), c.gamma[k], c.beta[k], A[k], S[k]);
     }
     if (!p.on) return;
 #pragma unroll

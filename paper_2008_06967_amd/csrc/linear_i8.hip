@@ -408,20 +408,18 @@ __global__ __launch_bounds__(kFewThreads) void linear_i8_few_kernel(LinArgs a, c
             const int k0 = 64 * (s0 + i) + 16 * grp;
             const bool in = s0 + i < s1 && k0 < a.kp;
             wf[i] = in ? *reinterpret_cast<const i32x4*>(wp + 64 * (s0 + i)) : zero;
-            const bool row = in && r16 < a.rows;
             constexpr int V = 16 / sizeof(TX);
+            const bool row = in && r16 < a.rows;
+            if (row && k0 + 16 <= ci) {
 #pragma unroll
-            for (int e = 0; e < 16; e += V) {
-                if (k0 + e + V <= ci) {
-                    QuLoose<TX, V> w = {};
-                    if (row) w = *reinterpret_cast<const QuLoose<TX, V>*>(xp + 64 * (s0 + i) + e);
+                for (int e = 0; e < 16; e += V) {
+                    const QuLoose<TX, V> w = *reinterpret_cast<const QuLoose<TX, V>*>(xp + 64 * (s0 + i) + e);
 #pragma unroll
                     for (int k = 0; k < V; ++k) v[i][e + k] = qu_float(w.e[k]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < V; ++k)
-                        v[i][e + k] = row && k0 + e + k < ci ? qu_float(xp[64 * (s0 + i) + e + k]) : 0.0f;
                 }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[i][e] = row && k0 + e < ci ? qu_float(xp[64 * (s0 + i) + e]) : 0.0f;
             }
         }
 #pragma unroll
