@@ -26,7 +26,7 @@ namespace {
 constexpr int kGnThreads = 256;      // of the two-launch form
 constexpr int kGnOneThreads = 512;   // of the one-launch form
 constexpr int kGnKeep = 16;          // vectors of a thread in the one-launch form, at most
-constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit
+constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit (2048: 154 us for 135)
 
 template <typename T, int N>
 struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) GnVec {
@@ -48,6 +48,7 @@ struct GnArgs {
     int slabs, pieces;               // slabs of a row; slabs of a group (1: whole groups in a slab)
     int chunks;
     int64_t chunk_rows;
+    int blocks, per_xcd;             // workgroups; of an XCD, in the one-launch form
     FastDiv by_chunks, by_slabs, by_pieces, by_c;
     FastDiv by_rows;                 // rows of a chunk
     FastDiv by_nv;                   // vectors of a full slab
@@ -399,9 +400,9 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
 }
 
 // Sums over the workgroup of each group's values, finished once a group: a
-// thread's per channel, then over the rows of its wave, then over waves and channels.  A wave holds
-// whole copies of the vectors' lanes (nvp of them, a power of two) or the
-// workgroup holds rows of several waves.
+// thread's per channel, then over the rows of its wave, then over waves and
+// channels.  nvp lanes (a power of two) hold a row: a wave several rows, or a
+// row several waves.
 template <int VEC, typename P, typename Finish>
 __device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int nvp, float (&v)[VEC], float* ent,
                                               float* res, Finish finish) {
@@ -438,7 +439,10 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     __shared__ float sums[kGnOneThreads * VEC];  // a slab's groups: at most its channels
     const int nv = (int)a.by_nv.d;
     const int shift = nv > 1 ? 32 - __builtin_clz(nv - 1) : 0, nvp = 1 << shift;     // lanes of a row
-    GnPlace<kGnOneThreads, VEC> p(a, (int)blockIdx.x);
+    // a cloud's slabs share lines of its rows: they go to one XCD
+    const int blk = (int)(blockIdx.x & 7) * a.per_xcd + (int)(blockIdx.x >> 3);
+    if (blk >= a.blocks) return;
+    GnPlace<kGnOneThreads, VEC> p(a, blk);
     p.slots = kGnOneThreads >> shift;
     p.slot = threadIdx.x >> shift;
     p.vec = threadIdx.x & (nvp - 1);
@@ -545,9 +549,11 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
         p.slabs = G * p.pieces;
     }
     const int64_t slots = std::max<int64_t>(1, kGnThreads / ceil_div(std::min<int64_t>(p.slab, C), vec));
-    // at most 128 chunks of a cloud, which every workgroup of the second launch joins, while a thread's chain of sums
-    // stays within 128 rows; at least 8 rows a thread
-    const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, kGnBlocks / std::max<int64_t>(1, B * p.slabs)));
+    // Every workgroup of the second launch joins all chunks of its cloud, 16 parts a thread at most: 256 chunks for 8
+    // groups (1 x 65536 x 64: 15 us, with 128 20), 128 for 32 (1 x 16384 x 256: 25 us, with 256 30).  A thread's chain
+    // of sums stays within 128 rows; at least 8 rows a thread.
+    const int64_t most_chunks = std::max<int64_t>(64, std::min<int64_t>(256, 4096 / std::max(1, p.slab / c)));
+    const int64_t want = std::min(most_chunks, std::max<int64_t>(1, kGnBlocks / std::max<int64_t>(1, B * p.slabs)));
     int64_t rows = std::max<int64_t>(ceil_div(N, want), 8 * slots);
     rows = std::max<int64_t>(std::min<int64_t>(rows, 128 * slots), ceil_div(N, 4096));
     p.chunk_rows = rows;
@@ -569,17 +575,16 @@ int group_norm_vec(int C, int G, int x_dtype) {
 
 template <typename TX, typename TY, int VEC, int ACT>
 void launch_group_norm(const GnArgs& a, const GnPlan& p, hipStream_t s) {
-    const int64_t blocks = a.B * a.slabs * a.chunks;
     if (p.keep) {
-        const dim3 grid((unsigned)blocks), block(kGnOneThreads);
+        const dim3 grid(8u * (unsigned)a.per_xcd), block(kGnOneThreads);
         if (p.keep < kGnKeep)
             gn_one_kernel<TX, TY, VEC, ACT, kGnKeep / 4><<<grid, block, 0, s>>>(a);
         else
             gn_one_kernel<TX, TY, VEC, ACT, kGnKeep><<<grid, block, 0, s>>>(a);
         return;
     }
-    gn_parts_kernel<TX, VEC><<<dim3((unsigned)blocks), dim3(kGnThreads), 0, s>>>(a);
-    gn_apply_kernel<TX, TY, VEC, ACT><<<dim3((unsigned)blocks), dim3(kGnThreads), 0, s>>>(a);
+    gn_parts_kernel<TX, VEC><<<dim3((unsigned)a.blocks), dim3(kGnThreads), 0, s>>>(a);
+    gn_apply_kernel<TX, TY, VEC, ACT><<<dim3((unsigned)a.blocks), dim3(kGnThreads), 0, s>>>(a);
 }
 
 template <typename TX, typename TY, int VEC>
@@ -637,10 +642,11 @@ extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype,
     MESO_REQUIRE(need == 0 || (ws && ws_bytes >= need), MESORASI_EWORKSPACE,
                  "mesorasi_group_norm: workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
     MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_group_norm: ws is not 16-byte aligned");
-    MESO_REQUIRE(B * p.slabs <= 0x7fffffff / p.chunks, MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
+    MESO_REQUIRE(B * p.slabs <= 0x7ffffff0 / p.chunks, MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
                  (long long)B, (long long)N);
+    const int blocks = (int)(B * p.slabs * p.chunks);
     const GnArgs a = {x, y, lens, gamma, beta, static_cast<float2*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,
-                      p.slab, p.slabs, p.pieces, p.chunks, p.chunk_rows, FastDiv(p.chunks), FastDiv(p.slabs),
+                      p.slab, p.slabs, p.pieces, p.chunks, p.chunk_rows, blocks, (int)ceil_div(blocks, 8), FastDiv(p.chunks), FastDiv(p.slabs),
                       FastDiv(p.pieces), FastDiv(C / G), FastDiv((unsigned)p.chunk_rows), FastDiv((unsigned)ceil_div(p.slab, vec))};
     hipStream_t s = as_stream(stream);
 #define MESO_GN(TX, TY, V)                                              \
