@@ -836,17 +836,31 @@ __global__ __launch_bounds__(kAtThreads, (DQ * RB > 2 ? 1 : 2)) void attention_f
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[j][q][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    for (int64_t j0 = begin + 16 * wave; j0 < end; j0 += 16 * W) {
+    f32x4 kn[4 * DQ], vn[4][DQ];
+    uint32_t bits_n = 0;
+    auto fetch = [&](int64_t j0) {
         const bool ok = j0 + l16 < end && (!mask || mask[j0 + l16]);
-        const uint32_t bits = (uint32_t)ballot(ok) & 0xffffu;
-        f32x4 kf[4 * DQ], vf[4][DQ];
+        bits_n = (uint32_t)ballot(ok) & 0xffffu;
 #pragma unroll
-        for (int i = 0; i < 4 * DQ; ++i) kf[i] = read4(kp + (j0 + l16) * a.kl, 16 * i + 4 * grp, ok);
+        for (int i = 0; i < 4 * DQ; ++i) kn[i] = read4(kp + (j0 + l16) * a.kl, 16 * i + 4 * grp, ok);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int q = 0; q < DQ; ++q)
-                vf[r][q] = read4(vp + (j0 + 4 * grp + r) * a.vl, 64 * q + 4 * l16, (bits >> (4 * grp + r)) & 1);
+                vn[r][q] = read4(vp + (j0 + 4 * grp + r) * a.vl, 64 * q + 4 * l16, (bits_n >> (4 * grp + r)) & 1);
+    };
+    if (begin + 16 * wave < end) fetch(begin + 16 * wave);
+    for (int64_t j0 = begin + 16 * wave; j0 < end; j0 += 16 * W) {
+        // the next block's rows come while this one's are multiplied
+        const uint32_t bits = bits_n;
+        f32x4 kf[4 * DQ], vf[4][DQ];
+#pragma unroll
+        for (int i = 0; i < 4 * DQ; ++i) kf[i] = kn[i];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int q = 0; q < DQ; ++q) vf[r][q] = vn[r][q];
+        if (j0 + 16 * W < end) fetch(j0 + 16 * W);
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
             f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
@@ -992,8 +1006,10 @@ AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int 
     p.Dp = (D + 31) / 32 * 32;
     p.splits = 1;
     p.rb = 0;
+    // Parts of 128 sources and up, and the launch that joins them, past 512 sources (2 x 12 heads over 722, fp32: 8.9 us
+    // in parts of 128, 10.5 of 256, 12.1 of 512; 3 x 12 queries over 486, bf16: 7.3 us whole, 8.5 in parts of 128).
     auto splits = [&](int64_t wg) {
-        return (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 256)));
+        return Nk <= 512 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 128)));
     };
     // Two blocks a wave read the sources' operands half as often (64 channels: 585 -> 564 us for 4 x 16384 over 4096, 8
     // heads) but above 64 channels leave one wave a SIMD (128: 1080 -> 1260 us).  Below a workgroup for most compute
