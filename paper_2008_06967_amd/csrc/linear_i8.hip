@@ -23,7 +23,7 @@ struct alignas(sizeof(T) * N) QuVec {
     T e[N];
 };
 
-// The same at any element: the hardware's loads need no more.
+// The same at any element: the hardware's loads and stores need no more.
 template <typename T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) QuLoose {
     T e[N];
@@ -163,7 +163,6 @@ struct LinArgs {
     int tiles_r, tiles_c;
     int64_t blocks;
     int per_xcd;
-    int vec;                         // rows of y take aligned runs of 4 channels
 };
 
 __device__ const uint4 kLinZero[1] = {};
@@ -184,7 +183,7 @@ template <typename TY>
 __device__ __forceinline__ void lin_out(const LinArgs& a, int64_t row, int ch, i32x4 acc, float xs,
                                         const float (&ws)[4], const float (&bs)[4]) {
     TY* y = static_cast<TY*>(a.y) + row * a.ldy + ch;
-    QuVec<TY, 4> v;
+    QuLoose<TY, 4> v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float f = ((float)acc[i] * xs) * ws[i] + bs[i];
@@ -194,8 +193,9 @@ __device__ __forceinline__ void lin_out(const LinArgs& a, int64_t row, int ch, i
         else
             v.e[i] = f32_to_bf16_any(f);
     }
-    if (a.vec && ch + 3 < a.co) {
-        *reinterpret_cast<QuVec<TY, 4>*>(y) = v;
+    if (ch + 3 < a.co) {
+        *reinterpret_cast<QuLoose<TY, 4>*>(y) = v;
+        asm volatile("");            // keeps this one store apart from those below
         return;
     }
 #pragma unroll
@@ -480,10 +480,12 @@ int run_linear(LinArgs& a, hipStream_t s) {
             linear_i8_few_kernel<int8_t, TY, 4><<<grid, block, 0, s>>>(a, nullptr, 0);
         return MESORASI_OK;
     }
-    // 256 x 256 tiles for many long products, else the largest tile that gives most compute units one: 16384 x 1024 ->
-    // 1024 takes 32.5 us in the first and 34.6 in the second, 16384 x 320 -> 256 9.2 in the second and 8.6 in the third,
-    // 65536 x 128 -> 128 17.0, 11.9 and 11.9, 4096 x 1024 -> 1024 27.5, 11.3 and 12.3
-    if (a.kp >= 1024 && ceil_div(a.rows, 256) * ceil_div(a.co, 256) >= 192) return launch_linear<TY, 2, 4, 4, 2>(a, s);
+    // 256 x 256 tiles for long products whose tiles fill at least three quarters of the compute units' turns, else the
+    // largest tile that gives most compute units one: 16384 x 1024 -> 1024 takes 32.5 us in the first and 34.6 in the
+    // second, 16384 x 320 -> 256 9.2 in the second and 8.6 in the third, 65536 x 128 -> 128 17.0, 11.9 and 11.9,
+    // 4096 x 1024 -> 1024 27.5, 11.3 and 12.3
+    const int64_t t = ceil_div(a.rows, 256) * ceil_div(a.co, 256);
+    if (a.kp >= 1024 && 4 * t >= 3 * 256 * ceil_div(t, 256)) return launch_linear<TY, 2, 4, 4, 2>(a, s);
     if (ceil_div(a.rows, 128) * ceil_div(a.co, 128) >= 192) return launch_linear<TY, 2, 4, 2, 1>(a, s);
     return launch_linear<TY, 2, 2, 1, 1>(a, s);
 }
@@ -556,7 +558,6 @@ extern "C" int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, 
     const int kp = (int)i8_pad(c_in);
     const bool f32 = y_dtype == MESORASI_F32;
     LinArgs a = {static_cast<const int8_t*>(x), x_scale, W, w_scale, bias, y, ld_x, ld_w, ld_y, rows, kp, c_out, relu};
-    a.vec = ld_y % 4 == 0 && aligned(y, f32 ? 16 : 8);
     if (linear_few_fused(rows, kp, x_dtype)) {
         if (x_dtype == MESORASI_F32) {
             const float* p = static_cast<const float*>(x);
