@@ -570,7 +570,8 @@ size_t mesorasi_group_norm_workspace(int64_t B, int64_t N, int32_t C, int32_t G,
  *   scale [rows] float32 out
  * Errors: EINVAL for NULL pointers, rows < 0, C < 1, ld_x < C, ld_q < C or
  *         not a multiple of 16, a misaligned q; EUNSUPPORTED for an unknown
- *         dtype, C > MESORASI_MAX_WIDTH_I8 or rows > 2^31 - 1.
+ *         dtype, C > MESORASI_MAX_WIDTH_I8, rows > 2^31 - 1 or more work than
+ *         one launch holds.
  */
 int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype, int64_t rows, int32_t C, int8_t* q,
                          int64_t ld_q, float* scale, void* stream);
@@ -599,8 +600,8 @@ int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype, int64_t r
  *         ld < width, an ld_w (or an I8 ld_x) that is no multiple of 16, a
  *         misaligned W, ws or I8 x, x_scale missing (I8) or given
  *         (F32, BF16); EUNSUPPORTED for an unknown dtype, a width above
- *         MESORASI_MAX_WIDTH_I8 or rows > 2^31 - 1; EWORKSPACE when ws is too
- *         small.
+ *         MESORASI_MAX_WIDTH_I8, rows > 2^31 - 1 or more work than one launch
+ *         holds; EWORKSPACE when ws is too small.
  */
 int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, const float* x_scale, int64_t rows, int32_t c_in,
                        const int8_t* W, int64_t ld_w, const float* w_scale, const float* bias, int32_t c_out,
@@ -629,8 +630,8 @@ size_t mesorasi_linear_i8_workspace(int64_t rows, int32_t c_in, int32_t c_out, i
  * Errors: EINVAL for NULL pointers, rows < 0, H < 1, D < 1, ld < width, a
  *         negative section, P < 1, 2 P > D, y == x with another leading
  *         dimension; EUNSUPPORTED for an unknown dtype, n_axes outside
- *         [1, MESORASI_MAX_AXES], D > MESORASI_MAX_D_ROTARY, H > 65536 or
- *         rows > 2^31 - 1.
+ *         [1, MESORASI_MAX_AXES], D > MESORASI_MAX_D_ROTARY, H > 65536, rows >
+ *         2^31 - 1 or more work than one launch holds.
  */
 int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t H, int32_t D, const float* pos,
                     int64_t ld_pos, int32_t n_axes, const int32_t* sections, const float* freq, int32_t interleaved,

@@ -466,7 +466,8 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
 // ---------------------------------------------------------------------------
 
 // v = hi + mid + lo, each in bf16: 8 bits each of a float's 24, with nothing
-// left over (values that bf16 rounds to infinity, above 3.39e38, aside).
+// left over -- of values from 2^-110 (below, the last parts may be denormal and
+// lost) to 3.38e38 (above, bf16 rounds to infinity).
 struct AtSplit {
     uint32_t hi, mid, lo;            // of two values
 };
@@ -1164,7 +1165,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     a.Dp = p.Dp;
     a.part = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
     const int64_t per = ceil_div(p.blocks, 8);
-    MESO_REQUIRE(per <= 0x7fffffff / 8, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
+    MESO_REQUIRE(launch_fits(8 * per, kAtThreads), MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
                  (long long)p.blocks);
     a.per_xcd = (int)per;
     // 16-byte pieces of every row, runs of 4 channels of the output

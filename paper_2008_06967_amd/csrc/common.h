@@ -24,6 +24,9 @@ inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// A launch holds fewer than 2^32 threads.
+inline bool launch_fits(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
+
 inline bool aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; }
 
 // Zero-fill of a strided [rows, cols] float32 region (used before pooled

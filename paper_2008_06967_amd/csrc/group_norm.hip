@@ -201,25 +201,29 @@ struct GnChannels {
     float ref[VEC], gamma[VEC], beta[VEC];
 };
 
-template <typename TX, int VEC, bool AFFINE, typename P>
+template <typename TX, int VEC, typename P>
 __device__ __forceinline__ void gn_channels(const GnArgs& a, const P& p, GnChannels<VEC>& c) {
     const TX* x0 = static_cast<const TX*>(a.x) + p.b * a.N * a.ldx + (int64_t)p.first * a.c;
     p.channel_groups(a, c.grp);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) c.ref[k] = 0.0f;
+    if (p.on && p.len > 0)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) c.ref[k] = gn_float(x0[c.grp[k] * a.c]);
+}
+
+template <int VEC, typename P>
+__device__ __forceinline__ void gn_affine(const GnArgs& a, const P& p, GnChannels<VEC>& c) {
     const int ch = p.ch0 + p.vec * VEC;
-    const bool any = p.on && p.len > 0;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-        c.ref[k] = 0.0f;
         c.gamma[k] = 1.0f;
         c.beta[k] = 0.0f;
     }
-    if (any)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) c.ref[k] = gn_float(x0[c.grp[k] * a.c]);
-    if (AFFINE && any && a.gamma)
+    if (p.on && a.gamma)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) c.gamma[k] = a.gamma[ch + k];
-    if (AFFINE && any && a.beta)
+    if (p.on && a.beta)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) c.beta[k] = a.beta[ch + k];
 }
@@ -257,7 +261,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_parts_kernel(GnArgs a) {
     const int nrows = (int)(r1 - r0);
     const bool merged = a.pieces > 1 || a.c % VEC == 0;
     GnChannels<VEC> c;
-    gn_channels<TX, VEC, false>(a, p, c);
+    gn_channels<TX, VEC>(a, p, c);
     float sum[VEC] = {}, sq[VEC] = {}, f[VEC] = {};
     const int full = nrows / p.slots, tail = nrows - full * p.slots;      // rows of every slot, slots with one more
     const int mine = p.on ? full + (p.slot < tail) : 0;
@@ -375,7 +379,8 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     GnChannels<VEC> c;
     float A[VEC] = {}, S[VEC] = {};
     if (r0 < p.len) {
-        gn_channels<TX, VEC, true>(a, p, c);
+        gn_channels<TX, VEC>(a, p, c);
+        gn_affine<VEC>(a, p, c);
         gn_join_chunks(a, p, stat);
         __syncthreads();
         if (p.on) {
@@ -431,6 +436,15 @@ __device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int n
     __syncthreads();
 }
 
+// Packed rows stay packed: what one pass unpacked is not kept for the next.
+template <typename T, int N>
+__device__ __forceinline__ void gn_keep(GnVec<T, N>& v) {
+    if constexpr (sizeof(T) == 2 && N == 8) {
+        uint4& r = reinterpret_cast<uint4&>(v);
+        asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));
+    }
+}
+
 // One launch: the slab's valid rows stay in registers between the
 // statistics and the output, so the variance is taken about the mean.
 template <typename TX, typename TY, int VEC, int ACT, int KEEP>
@@ -452,7 +466,8 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     const TX* __restrict__ xp = static_cast<const TX*>(a.x) + (p.b * a.N + p.slot) * a.ldx + p.ch0 + p.vec * VEC;
     TY* __restrict__ yp = static_cast<TY*>(a.y) + (p.b * a.N + p.slot) * a.ldy + p.ch0 + p.vec * VEC;
     GnChannels<VEC> c;
-    gn_channels<TX, VEC, true>(a, p, c);
+    gn_channels<TX, VEC>(a, p, c);
+    if (KEEP < kGnKeep) gn_affine<VEC>(a, p, c);       // the long form has no registers for them yet
     GnVec<TX, VEC> w[KEEP];
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
@@ -474,12 +489,15 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
-            if (i < mine)
+            if (i < mine) {
+                gn_keep(w[i]);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     const float d = (gn_float(w[i].e[k]) - c.ref[k]) - mean[k];
                     v[k] = fmaf(d, d, v[k]);
                 }
+            }
+        if (KEEP == kGnKeep) gn_affine<VEC>(a, p, c);
         gn_group_sums<VEC>(a, p, nvp, v, ent, sums, [&](float sum) { return 1.0f / sqrtf(sum * inv + a.eps); });
 #pragma unroll
         for (int k = 0; k < VEC; ++k) gn_factor(make_float2(mean[k], sums[c.grp[k]]), c.gamma[k], c.beta[k], A[k], S[k]);
@@ -488,6 +506,7 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
         if (i < mine) {
+            gn_keep(w[i]);
             GnVec<TY, VEC> o;
 #pragma unroll
             for (int k = 0; k < VEC; ++k)
@@ -642,7 +661,7 @@ extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype,
     MESO_REQUIRE(need == 0 || (ws && ws_bytes >= need), MESORASI_EWORKSPACE,
                  "mesorasi_group_norm: workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
     MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_group_norm: ws is not 16-byte aligned");
-    MESO_REQUIRE(B * p.slabs <= 0x7ffffff0 / p.chunks, MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
+    MESO_REQUIRE(launch_fits(ceil_div(B * p.slabs * p.chunks, 8) * 8, p.keep ? kGnOneThreads : kGnThreads), MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
                  (long long)B, (long long)N);
     const int blocks = (int)(B * p.slabs * p.chunks);
     const GnArgs a = {x, y, lens, gamma, beta, static_cast<float2*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,

@@ -126,11 +126,19 @@ __global__ __launch_bounds__(kQuThreads) void quantize_i8_kernel(const T* __rest
     }
 }
 
+// Lanes of a row: as few as keep it in registers, so that short rows share a wave.
+int quantize_lanes(int C, int dtype) {
+    const int nv = ((C + 15) & ~15) / (dtype == MESORASI_F32 ? 4 : 8);
+    return nv <= 4 * kQuKeep ? 4 : nv <= 16 * kQuKeep ? 16 : 64;
+}
+
+bool quantize_fits(int64_t rows, int C, int dtype) {
+    return launch_fits(ceil_div(rows, kQuThreads / quantize_lanes(C, dtype)), kQuThreads);
+}
+
 template <typename T>
 void run_quantize(const T* x, int64_t ldx, int64_t rows, int C, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
-    const int nv = ((C + 15) & ~15) / (16 / (int)sizeof(T));
-    // as few lanes as keep a row in registers, so that short rows share a wave
-    const int lpr = nv <= 4 * kQuKeep ? 4 : nv <= 16 * kQuKeep ? 16 : 64;
+    const int lpr = quantize_lanes(C, sizeof(T) == 4 ? MESORASI_F32 : MESORASI_BF16);
     const dim3 grid((unsigned)ceil_div(rows, kQuThreads / lpr)), block(kQuThreads);
     switch (lpr) {
         case 4: quantize_i8_kernel<T, 4><<<grid, block, 0, s>>>(x, ldx, rows, C, q, ldq, scale); break;
@@ -344,8 +352,6 @@ int launch_linear(LinArgs& a, hipStream_t s) {
     a.tiles_c = (int)ceil_div(a.co, TC);
     a.blocks = (int64_t)a.tiles_r * a.tiles_c;
     const int64_t per = ceil_div(a.blocks, 8);
-    MESO_REQUIRE(per <= 0x7fffffff / 8, MESORASI_EUNSUPPORTED, "mesorasi_linear_i8: %lld workgroups",
-                 (long long)a.blocks);
     a.per_xcd = (int)per;
     linear_i8_kernel<TY, WC, WR, BC, BR><<<dim3((unsigned)(8 * per)), dim3(64 * WC * WR), bytes, s>>>(a);
     return MESORASI_OK;
@@ -516,8 +522,8 @@ extern "C" int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype
                  "mesorasi_quantize_i8: ld_q = %lld (at least C and a multiple of 16)", (long long)ld_q);
     MESO_REQUIRE(x_dtype == MESORASI_F32 || x_dtype == MESORASI_BF16, MESORASI_EUNSUPPORTED,
                  "mesorasi_quantize_i8: dtype %d", x_dtype);
-    MESO_REQUIRE(C <= MESORASI_MAX_WIDTH_I8 && rows <= 0x7fffffff, MESORASI_EUNSUPPORTED,
-                 "mesorasi_quantize_i8: C = %d, rows = %lld", C, (long long)rows);
+    MESO_REQUIRE(C <= MESORASI_MAX_WIDTH_I8 && rows <= 0x7fffffff && quantize_fits(rows, C, x_dtype),
+                 MESORASI_EUNSUPPORTED, "mesorasi_quantize_i8: C = %d, rows = %lld", C, (long long)rows);
     if (rows == 0) return MESORASI_OK;
     MESO_REQUIRE(x && q && scale, MESORASI_EINVAL, "mesorasi_quantize_i8: NULL pointer");
     MESO_REQUIRE(aligned(q, 16), MESORASI_EINVAL, "mesorasi_quantize_i8: q is not 16-byte aligned");
@@ -545,7 +551,10 @@ extern "C" int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, 
                  MESORASI_EUNSUPPORTED, "mesorasi_linear_i8: dtypes %d, %d", x_dtype, y_dtype);
     MESO_REQUIRE(ld_w % 16 == 0 && (x_dtype != MESORASI_I8 || ld_x % 16 == 0), MESORASI_EINVAL,
                  "mesorasi_linear_i8: an 8-bit leading dimension is no multiple of 16");
-    MESO_REQUIRE(c_in <= MESORASI_MAX_WIDTH_I8 && c_out <= MESORASI_MAX_WIDTH_I8 && rows <= 0x7fffffff,
+    // tiles of 128 x 128 in the most workgroups that many rows and channels get
+    MESO_REQUIRE(c_in <= MESORASI_MAX_WIDTH_I8 && c_out <= MESORASI_MAX_WIDTH_I8 && rows <= 0x7fffffff &&
+                     launch_fits(ceil_div(rows, 128) * ceil_div(c_out, 128) + 7, 512) &&
+                     (x_dtype == MESORASI_I8 || quantize_fits(rows, c_in, x_dtype)),
                  MESORASI_EUNSUPPORTED, "mesorasi_linear_i8: c_in = %d, c_out = %d, rows = %lld", c_in, c_out,
                  (long long)rows);
     if (rows == 0) return MESORASI_OK;

@@ -208,6 +208,8 @@ extern "C" int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64
     while (tpr < kRotThreads && tpr < (int64_t)H * ih) tpr *= 2;
     a.R = R;
     a.tpr = tpr;
+    MESO_REQUIRE(launch_fits(ceil_div(rows, R), kRotThreads), MESORASI_EUNSUPPORTED, "mesorasi_rotary: %lld rows of %lld pairs",
+                 (long long)rows, (long long)P);
     const unsigned grid = (unsigned)ceil_div(rows, R);
     hipStream_t s = as_stream(stream);
     if (dtype == MESORASI_F32) {

@@ -592,6 +592,8 @@ def _ld(t: torch.Tensor, name: str):
     """(pointer, leading dimension) of rows, which must collapse; the stride
     of a single row is not used."""
     _require(t.dim() >= 2 and (t.shape[-1] <= 1 or t.stride(-1) == 1), f"{name}'s last dimension must be contiguous")
+    if t.numel() == 0:
+        return t.data_ptr(), t.shape[-1]
     n, ld = 1, None
     for d in range(t.dim() - 2, -1, -1):
         if t.shape[d] == 1:
@@ -600,7 +602,7 @@ def _ld(t: torch.Tensor, name: str):
             ld = t.stride(d)
         _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
         n *= t.shape[d]
-    return t.data_ptr(), t.shape[-1] if ld is None or n == 0 else ld
+    return t.data_ptr(), t.shape[-1] if ld is None else ld
 
 
 def group_norm_workspace_bytes(B: int, N: int, C: int, G: int, dtype: int = F32) -> int:
@@ -661,7 +663,7 @@ def _ld_int8(t: torch.Tensor, name: str):
     p, ld = _ld(t, name)
     C = t.shape[-1]
     pad = (C + 15) // 16 * 16
-    if ld == C and ld % 16 and t.numel() == C:
+    if ld == C and ld % 16 and t.numel() in (0, C):
         ld = pad
     if t.numel() and ld % 16 == 0:
         have = t.untyped_storage().nbytes() - t.storage_offset()
@@ -791,7 +793,9 @@ def rotary(x: torch.Tensor, pos: torch.Tensor, p: RotaryParams, out: torch.Tenso
 def _heads(t: torch.Tensor, name: str):
     """(pointer, leading dimension) of [..., H, D] rows of heads side by side."""
     H, D = t.shape[-2], t.shape[-1]
-    _require((D <= 1 or t.stride(-1) == 1) and (H <= 1 or t.stride(-2) == D), f"{name}'s heads must lie side by side")
+    _require(t.numel() == 0 or ((D <= 1 or t.stride(-1) == 1) and (H <= 1 or t.stride(-2) == D)), f"{name}'s heads must lie side by side")
+    if t.numel() == 0:
+        return t.data_ptr(), H * D
     n, ld = 1, None
     for d in range(t.dim() - 3, -1, -1):
         if t.shape[d] == 1:
@@ -800,7 +804,7 @@ def _heads(t: torch.Tensor, name: str):
             ld = t.stride(d)
         _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
         n *= t.shape[d]
-    return t.data_ptr(), H * D if ld is None or n == 0 else ld
+    return t.data_ptr(), H * D if ld is None else ld
 
 
 def cross_attention_workspace_bytes(B: int, Nq: int, Nk: int, Hq: int, Hkv: int, D: int, dtype: int = F32) -> int:

@@ -469,3 +469,19 @@ def test_cross_attention_validation_and_workspace():
     assert st(f, *args(q=NULL, o=NULL, Nq=0)) == _lib.OK
     assert L.mesorasi_cross_attention_workspace(2, 4, 16, 4, 3, 64, 1) == 0
     assert L.mesorasi_cross_attention_workspace(2, -4, 16, 4, 2, 64, 1) == 0
+
+
+def test_more_work_than_one_launch_holds():
+    """2^32 threads and up are refused before any HIP call."""
+    big = 0x7fffffff
+    assert st("mesorasi_quantize_i8", FAKE, 8192, 0, big, 8192, FAKE, 8192, FAKE, NULL) == _lib.EUNSUPPORTED
+    for xd, xs in ((2, FAKE), (0, NULL)):
+        assert st("mesorasi_linear_i8", FAKE, 64, xd, xs, big, 64, FAKE, 64, FAKE, NULL, 4096, 0, FAKE, 4096, 0, FAKE,
+                  1 << 60, NULL) == _lib.EUNSUPPORTED
+    S = (ctypes.c_int32 * 1)(512)
+    assert st("mesorasi_rotary", FAKE, 1024, 0, big, 1, 1024, FAKE, 1, 1, S, FAKE, 0, ctypes.c_void_p(0x2000), 1024,
+              NULL) == _lib.EUNSUPPORTED
+    assert st("mesorasi_group_norm", FAKE, 64, 0, 1 << 28, 1, 64, 64, NULL, NULL, NULL, 1e-5, 0, FAKE, 64, 0, FAKE,
+              1 << 60, NULL) == _lib.EUNSUPPORTED
+    assert st("mesorasi_cross_attention", FAKE, 64, 64, 64, FAKE, 64, 64, 64, FAKE, 64, 64, 64, 1, 1 << 30, 1, 1, 1, 1,
+              64, 1.0, NULL, NULL, 0, FAKE, 64, 64, 64, FAKE, 1 << 60, NULL) == _lib.EUNSUPPORTED

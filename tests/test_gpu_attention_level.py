@@ -521,6 +521,22 @@ def test_attention_nan_query(gpu, dtype):
     assert torch.equal(got, ref)
 
 
+def test_empty_inputs(gpu):
+    """No rows, no points, no clouds: empty results of the right shapes."""
+    p = ops.Int8Params.from_float(torch.ones((4, 5), device="cuda"))
+    r = ops.RotaryParams([2])
+    for lead in ((0,), (0, 3), (2, 0)):
+        x = torch.zeros(lead + (5,), device="cuda")
+        assert tuple(ops.linear_int8(x, p).shape) == lead + (4,)
+        q, s = ops.quantize_int8(x)
+        assert tuple(q.shape) == lead + (5,) and tuple(s.shape) == lead
+        assert tuple(ops.linear_int8(q, p, x_scale=s).shape) == lead + (4,)
+        z = torch.zeros(lead + (3, 6), device="cuda")
+        assert ops.rotary(z, torch.zeros(lead + (1,), device="cuda"), r).shape == z.shape
+    for shape in ((0, 5, 8), (3, 0, 8)):
+        assert tuple(ops.group_norm(torch.zeros(shape, device="cuda"), 2).shape) == shape
+
+
 # ---------------------------------------------------------------------------
 # together, streams, graphs
 # ---------------------------------------------------------------------------
