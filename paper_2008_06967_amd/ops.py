@@ -550,28 +550,32 @@ def _dtype(t: torch.Tensor, name: str) -> int:
 
 def _like(t, x: torch.Tensor, name: str, dtype, shape):
     """t (may be None) is a contiguous tensor of this dtype and shape on x's device."""
-    if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()
-                              and t.device == x.device):
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == x.device):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {x.device}")
 
 
 _entry_points: dict = {}
+_this_device = torch._C._cuda_getDevice
+_this_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _entry(name: str):
+    fn = _entry_points.get(name)
+    if fn is None:
+        fn = _entry_points[name] = getattr(_lib.lib(), "mesorasi_" + name)
+    return fn
 
 
 def _call(x: torch.Tensor, where: str, *args):
     """The entry point `where` on x's device, on that device's current stream."""
-    dev = x.device
-    if dev.type != "cuda":
-        raise ValueError(f"{where}: tensors must be on a GPU, not on {dev}")
-    fn = _entry_points.get(where)
-    if fn is None:
-        fn = _entry_points[where] = getattr(_lib.lib(), "mesorasi_" + where)
-    i = dev.index
-    if i == torch._C._cuda_getDevice():
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if not x.is_cuda:
+        raise ValueError(f"{where}: tensors must be on a GPU, not on {x.device}")
+    fn, i = _entry(where), x.get_device()
+    if i == _this_device():
+        rc = fn(*args, _this_stream(i))
     else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+        with torch.cuda.device(i):
+            rc = fn(*args, _this_stream(i))
     if rc:
         check(rc, where)
 
@@ -581,28 +585,43 @@ def _workspace(x: torch.Tensor, need: int, ws):
     when it is missing or too small."""
     if not need:
         return None, 0, None
-    _require(ws is None or (ws.device == x.device and ws.dtype == torch.uint8 and ws.is_contiguous()),
-             f"ws must be a contiguous uint8 tensor on {x.device}")
+    if ws is not None and not (ws.device == x.device and ws.dtype is torch.uint8 and ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {x.device}")
     if ws is None or ws.numel() < need:
         ws = torch.empty(need, dtype=torch.uint8, device=x.device)
     return ws.data_ptr(), ws.numel(), ws
 
 
-def _ld(t: torch.Tensor, name: str):
-    """(pointer, leading dimension) of rows, which must collapse; the stride
-    of a single row is not used."""
-    _require(t.dim() >= 2 and (t.shape[-1] <= 1 or t.stride(-1) == 1), f"{name}'s last dimension must be contiguous")
-    if t.numel() == 0:
-        return t.data_ptr(), t.shape[-1]
+def _new(x: torch.Tensor, shape, dtype=None) -> torch.Tensor:
+    """An uninitialised contiguous tensor on x's device, of x's type unless given."""
+    return x.new_empty(shape, dtype=dtype)
+
+
+def _collapsed(shape, stride, last: int, name: str):
+    """The row stride of dimensions 0 .. last, which must collapse into rows;
+    None for a single row, whose stride is not used."""
     n, ld = 1, None
-    for d in range(t.dim() - 2, -1, -1):
-        if t.shape[d] == 1:
+    for d in range(last, -1, -1):
+        if shape[d] == 1:
             continue
         if ld is None:
-            ld = t.stride(d)
-        _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
-        n *= t.shape[d]
-    return t.data_ptr(), t.shape[-1] if ld is None else ld
+            ld = stride[d]
+        if stride[d] != ld * n:
+            raise ValueError(f"{name}'s leading dimensions must collapse into rows")
+        n *= shape[d]
+    return ld
+
+
+def _ld(t: torch.Tensor, name: str):
+    """(pointer, leading dimension) of rows of the last dimension."""
+    shape = t.shape
+    if t.is_contiguous() and len(shape) >= 2:
+        return t.data_ptr(), shape[-1]
+    stride = t.stride()
+    if len(shape) < 2 or (shape[-1] > 1 and stride[-1] != 1):
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    ld = _collapsed(shape, stride, len(shape) - 2, name)
+    return t.data_ptr(), shape[-1] if ld is None else ld
 
 
 def group_norm_workspace_bytes(B: int, N: int, C: int, G: int, dtype: int = F32) -> int:
@@ -617,21 +636,24 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
     [C] float32; lens [B] int32 (rows from lens[b] on are not read and come
     out 0).  out: like x, or of the other type (see the C header)."""
     _require(x.dim() == 3, "x must be [B, N, C]")
-    _require(act in _ACTS, f"act must be one of {sorted(_ACTS)}")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}")
     B, N, C = x.shape
-    dt = _dtype(x, "x")
+    dt = dy = _dtype(x, "x")
     _like(gamma, x, "gamma", torch.float32, (C,))
     _like(beta, x, "beta", torch.float32, (C,))
     _like(lens, x, "lens", torch.int32, (B,))
-    if out is None:
-        out = torch.empty((B, N, C), dtype=x.dtype, device=x.device)
-    else:
-        _require(tuple(out.shape) == (B, N, C) and out.device == x.device, "out must have x's shape and device")
     px, ldx = _ld(x, "x")
-    py, ldy = _ld(out, "out")
-    wp, wn, ws = _workspace(x, group_norm_workspace_bytes(B, N, C, groups, dt), ws)
+    if out is None:
+        out = _new(x, (B, N, C))
+        py, ldy = out.data_ptr(), C
+    else:
+        _require(out.shape == x.shape and out.device == x.device, "out must have x's shape and device")
+        dy = _dtype(out, "out")
+        py, ldy = _ld(out, "out")
+    wp, wn, ws = _workspace(x, _entry("group_norm_workspace")(B, N, C, groups, dt), ws)
     _call(x, "group_norm", px, ldx, dt, B, N, C, groups, _ptr(lens), _ptr(gamma), _ptr(beta), eps, _ACTS[act], py, ldy,
-          _dtype(out, "out"), wp, wn)
+          dy, wp, wn)
     return out
 
 
@@ -641,15 +663,15 @@ def quantize_int8(x: torch.Tensor, out: torch.Tensor | None = None, scale: torch
     linear_int8 reads them."""
     dt = _dtype(x, "x")
     px, ldx = _ld(x, "x")
-    C, lead = x.shape[-1], tuple(x.shape[:-1])
+    C, lead = x.shape[-1], x.shape[:-1]
     rows = math.prod(lead)
     if out is None:
-        out = torch.empty(lead + ((C + 15) // 16 * 16,), dtype=torch.int8, device=x.device)[..., :C]
+        out = _new(x, (*lead, (C + 15) // 16 * 16), torch.int8)[..., :C]
     else:
         _require(out.dtype == torch.int8 and out.shape == x.shape and out.device == x.device,
                  "out must be int8 of x's shape, on x's device")
     if scale is None:
-        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+        scale = _new(x, lead, torch.float32)
     else:
         _like(scale, x, "scale", torch.float32, lead)
     pq, ldq = _ld_int8(out, "out")
@@ -665,10 +687,10 @@ def _ld_int8(t: torch.Tensor, name: str):
     pad = (C + 15) // 16 * 16
     if ld == C and ld % 16 and t.numel() in (0, C):
         ld = pad
-    if t.numel() and ld % 16 == 0:
+    if pad != C and t.numel() and ld % 16 == 0:
         have = t.untyped_storage().nbytes() - t.storage_offset()
-        _require((t.numel() // C - 1) * ld + pad <= have,
-                 f"{name}'s last row must be followed by its padding to 16 bytes")
+        if (t.numel() // C - 1) * ld + pad > have:
+            raise ValueError(f"{name}'s last row must be followed by its padding to 16 bytes")
     return p, ld
 
 
@@ -701,6 +723,7 @@ class Int8Params:
         if bias is not None:
             self.bias = torch.as_tensor(bias).to(device=device, dtype=torch.float32).reshape(-1).contiguous()
             _require(self.bias.numel() == self.c_out, "bias must hold one value for each output channel")
+        self.abi = (self.W.data_ptr(), self.ld, self.w_scale.data_ptr(), _ptr(self.bias), self.c_out)
 
     @classmethod
     def from_float(cls, W, bias=None, device="cuda"):
@@ -722,12 +745,13 @@ def linear_int8(x: torch.Tensor, p: Int8Params, x_scale: torch.Tensor | None = N
     bfloat16 (brought to 8 bits within the call), or int8 rows of
     quantize_int8() with their x_scale.  out_dtype: float32 (the default) or
     bfloat16."""
-    int8 = x.dtype == torch.int8
+    int8 = x.dtype is torch.int8
     dt = I8 if int8 else _dtype(x, "x")
-    if x.shape[-1] != p.c_in:
-        raise ValueError(f"x has {x.shape[-1]} columns, the weights {p.c_in}")
+    *lead, c_in = x.shape
+    if c_in != p.c_in:
+        raise ValueError(f"x has {c_in} columns, the weights {p.c_in}")
     _require(p.W.device == x.device, "the weights are on another device than x")
-    lead = tuple(x.shape[:-1])
+    lead = tuple(lead)
     rows = math.prod(lead)
     _require(int8 == (x_scale is not None), "x_scale goes with int8 rows, and only with them")
     if int8:
@@ -736,14 +760,15 @@ def linear_int8(x: torch.Tensor, p: Int8Params, x_scale: torch.Tensor | None = N
     else:
         px, ldx = _ld(x, "x")
     if out is None:
-        out = torch.empty(lead + (p.c_out,), dtype=out_dtype or torch.float32, device=x.device)
+        out = _new(x, lead + (p.c_out,), out_dtype or torch.float32)
+        py, ldy = out.data_ptr(), p.c_out
     else:
-        _require(tuple(out.shape) == lead + (p.c_out,) and out.device == x.device
-                 and out_dtype in (None, out.dtype), "out must be [..., C_out] of out_dtype on x's device")
-    py, ldy = _ld(out, "out")
-    wp, wn, ws = _workspace(x, linear_int8_workspace_bytes(rows, p, dt), ws)
-    _call(x, "linear_i8", px, ldx, dt, _ptr(x_scale), rows, p.c_in, p.W.data_ptr(), p.ld, p.w_scale.data_ptr(),
-          _ptr(p.bias), p.c_out, 1 if relu else 0, py, ldy, _dtype(out, "out"), wp, wn)
+        _require(out.shape == lead + (p.c_out,) and out.device == x.device and out_dtype in (None, out.dtype),
+                 "out must be [..., C_out] of out_dtype on x's device")
+        py, ldy = _ld(out, "out")
+    wp, wn, ws = _workspace(x, _entry("linear_i8_workspace")(rows, c_in, p.c_out, dt), ws)
+    _call(x, "linear_i8", px, ldx, dt, _ptr(x_scale), rows, c_in, *p.abi, 1 if relu else 0, py, ldy,
+          _dtype(out, "out"), wp, wn)
     return out
 
 
@@ -771,39 +796,36 @@ def rotary(x: torch.Tensor, pos: torch.Tensor, p: RotaryParams, out: torch.Tenso
     D] float32 or bfloat16, heads side by side; pos [..., axes] float32.  out
     may be x."""
     dt = _dtype(x, "x")
-    _require(x.dim() >= 2, "x must be [..., H, D]")
-    H, D = x.shape[-2], x.shape[-1]
-    lead = tuple(x.shape[:-2])
-    if pos.dtype != torch.float32 or tuple(pos.shape) != lead + (len(p.sections),) or pos.device != x.device:
-        raise ValueError(f"pos must be float32 {list(lead) + [len(p.sections)]} on {x.device}")
+    shape = x.shape
+    _require(len(shape) >= 2, "x must be [..., H, D]")
+    *lead, H, D = shape
+    axes = len(p.sections)
+    if pos.dtype is not torch.float32 or pos.shape != (*lead, axes) or pos.device != x.device:
+        raise ValueError(f"pos must be float32 {lead + [axes]} on {x.device}")
     _require(p.freq.device == x.device, "the frequencies are on another device than x")
-    if out is None:
-        out = torch.empty(lead + (H, D), dtype=x.dtype, device=x.device)
-    else:
-        _require(out.dtype == x.dtype and out.shape == x.shape and out.device == x.device, "out must be like x")
-    rows = math.prod(lead)
     px, ldx = _heads(x, "x")
-    py, ldy = _heads(out, "out")
-    pp, ldp = _ld(pos if pos.dim() >= 2 else pos[None], "pos")
-    _call(x, "rotary", px, ldx, dt, rows, H, D, pp, ldp, len(p.sections), p._sections_c, p.freq.data_ptr(),
+    if out is None:
+        out = _new(x, shape)
+        py, ldy = out.data_ptr(), H * D
+    else:
+        _require(out.dtype == x.dtype and out.shape == shape and out.device == x.device, "out must be like x")
+        py, ldy = _heads(out, "out")
+    pp, ldp = _ld(pos if lead else pos[None], "pos")
+    _call(x, "rotary", px, ldx, dt, math.prod(lead), H, D, pp, ldp, axes, p._sections_c, p.freq.data_ptr(),
           1 if p.interleaved else 0, py, ldy)
     return out
 
 
 def _heads(t: torch.Tensor, name: str):
     """(pointer, leading dimension) of [..., H, D] rows of heads side by side."""
-    H, D = t.shape[-2], t.shape[-1]
-    _require(t.numel() == 0 or ((D <= 1 or t.stride(-1) == 1) and (H <= 1 or t.stride(-2) == D)), f"{name}'s heads must lie side by side")
-    if t.numel() == 0:
+    shape = t.shape
+    H, D = shape[-2], shape[-1]
+    if t.is_contiguous():
         return t.data_ptr(), H * D
-    n, ld = 1, None
-    for d in range(t.dim() - 3, -1, -1):
-        if t.shape[d] == 1:
-            continue
-        if ld is None:
-            ld = t.stride(d)
-        _require(t.stride(d) == ld * n, f"{name}'s leading dimensions must collapse into rows")
-        n *= t.shape[d]
+    stride = t.stride()
+    if (D > 1 and stride[-1] != 1) or (H > 1 and stride[-2] != D):
+        raise ValueError(f"{name}'s heads must lie side by side")
+    ld = _collapsed(shape, stride, len(shape) - 3, name)
     return t.data_ptr(), H * D if ld is None else ld
 
 
@@ -811,11 +833,12 @@ def cross_attention_workspace_bytes(B: int, Nq: int, Nk: int, Hq: int, Hkv: int,
     return int(_lib.lib().mesorasi_cross_attention_workspace(B, Nq, Nk, Hq, Hkv, D, dtype))
 
 
-def _strides(t: torch.Tensor, name: str):
-    """Cloud, point and head strides; those of single entries are not used."""
-    D = t.shape[3]
-    _require(D <= 1 or t.stride(3) == 1, f"{name}'s channels must be contiguous")
-    return tuple(t.stride(d) if t.shape[d] > 1 else 0 for d in range(3))
+def _strides(t: torch.Tensor, shape, name: str):
+    """Pointer, cloud, point and head strides; those of single entries are not used."""
+    b, n, h, c = t.stride()
+    if c != 1 and shape[3] > 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+    return t.data_ptr(), b if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0
 
 
 def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: torch.Tensor | None = None,
@@ -828,28 +851,31 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     sources from k_len[b] on are not valid; k_mask [B, Nk] bool: only the True
     ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
     unless given.  out: like q (its strides may differ)."""
-    _require(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
-    B, Nq, Hq, D = q.shape
-    Nk, Hkv = k.shape[1], k.shape[2]
-    _require(k.shape[0] == B and k.shape[3] == D, "q, k and v must agree in B and D")
-    _require(k.dtype == q.dtype and v.dtype == q.dtype and k.device == q.device and v.device == q.device,
+    qs, ks = q.shape, k.shape
+    _require(len(qs) == 4 and len(ks) == 4 and v.shape == ks, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
+    B, Nq, Hq, D = qs
+    Nk, Hkv = ks[1], ks[2]
+    _require(ks[0] == B and ks[3] == D, "q, k and v must agree in B and D")
+    dev, qd = q.device, q.dtype
+    _require(k.dtype is qd and v.dtype is qd and k.device == dev and v.device == dev,
              "q, k and v must have one type and device")
     dt = _dtype(q, "q")
     _like(k_len, q, "k_len", torch.int32, (B,))
     mask_ld = 0
     if k_mask is not None:
-        if not (k_mask.dtype in (torch.bool, torch.uint8) and tuple(k_mask.shape) == (B, Nk)
-                and k_mask.device == q.device and (Nk <= 1 or k_mask.stride(1) == 1)):
-            raise ValueError(f"k_mask must be bool [{B}, {Nk}] with contiguous rows on {q.device}")
+        if not (k_mask.dtype in (torch.bool, torch.uint8) and k_mask.shape == (B, Nk) and k_mask.device == dev
+                and (Nk <= 1 or k_mask.stride(1) == 1)):
+            raise ValueError(f"k_mask must be bool [{B}, {Nk}] with contiguous rows on {dev}")
         mask_ld = k_mask.stride(0) if B > 1 else Nk
     if scale is None:
         scale = 1.0 / math.sqrt(D) if D else 1.0
     if out is None:
-        out = torch.empty((B, Nq, Hq, D), dtype=q.dtype, device=q.device)
+        out = _new(q, qs)
+        po = (out.data_ptr(), max(Nq, 1) * Hq * D, Hq * D, D)
     else:
-        _require(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out must be like q")
-    wp, wn, ws = _workspace(q, cross_attention_workspace_bytes(B, Nq, Nk, Hq, Hkv, D, dt), ws)
-    _call(q, "cross_attention", q.data_ptr(), *_strides(q, "q"), k.data_ptr(), *_strides(k, "k"), v.data_ptr(),
-          *_strides(v, "v"), dt, B, Nq, Nk, Hq, Hkv, D, scale, _ptr(k_len), _ptr(k_mask), mask_ld, out.data_ptr(),
-          *_strides(out, "out"), wp, wn)
+        _require(out.shape == qs and out.dtype is qd and out.device == dev, "out must be like q")
+        po = _strides(out, qs, "out")
+    wp, wn, ws = _workspace(q, _entry("cross_attention_workspace")(B, Nq, Nk, Hq, Hkv, D, dt), ws)
+    _call(q, "cross_attention", *_strides(q, qs, "q"), *_strides(k, ks, "k"), *_strides(v, ks, "v"), dt, B, Nq, Nk,
+          Hq, Hkv, D, scale, _ptr(k_len), _ptr(k_mask), mask_ld, *po, wp, wn)
     return out
