@@ -646,9 +646,12 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
         const char* tk = lds;
         const char* tv = lds + 3 * P::kPart;
 
+        // One block of 32 sources after another, so that a block's weights form between the products of its neighbors:
+        // scores 0, scores 1 with weights 0, outputs 0 with weights 1, outputs 1.
         f32x16 s[NB];
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
+        bf16x8 pb[2][3];
+        float f;
+        auto scores = [&](int kb) {
             const char* base = tk + (32 * kb + col) * CH * 16;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.0f;
@@ -665,50 +668,59 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
                 if (st + 1 < 2 * DB) read_k(st + 1);
                 s[kb] = at_mfma6(kf[st & 1], qf[st], s[kb]);
             }
-        }
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
+        };
+        auto drop = [&](int kb) {            // sources that are not valid
             const uint32_t w32 = (uint32_t)(cur >> (32 * kb));
             if (w32 != 0xffffffffu) {
                 const uint32_t w = w32 >> (4 * half);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[kb][r] = (w >> (8 * (r / 4) + r % 4)) & 1 ? s[kb][r] : -INFINITY;
             }
-        }
-        float mx = -INFINITY;
+        };
+        // weights in three parts, and the factor f of what was summed before: a query's reference m moves when its
+        // maximum passes it by 8
+        auto weights = [&](int kb, bf16x8 (&p)[2][3]) {
+            float mx = s[kb][0];
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-        float lo;
-        const float hi = at_other_half(mx, lo);
-        mx = fmaxf(lo, hi) * c;
-        if (ballot(mx > m + 8.0f)) {
-            const float mn = fmaxf(m, mx);
-            const float f = mn == -INFINITY ? 1.0f : at_exp2(m - mn);
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+            float lo;
+            const float hi = at_other_half(mx, lo);
+            mx = fmaxf(lo, hi) * c;
+            const float mn = mx > m + 8.0f ? mx : m;
+            f = mn == m ? 1.0f : at_exp2(m - mn);
             m = mn;
-            l *= f;
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
-        }
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
+            const float base = m == -INFINITY ? 0.0f : m;
+            float sum = 0.0f;
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                // this step's 16 weights, sources 16 st + 8 (e / 4) + 4 half + e % 4
+                // a step's 16 weights: sources 16 st + 8 (e / 4) + 4 half + e % 4
                 float pf[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) pf[e] = at_exp2(fmaf(s[kb][8 * st + e], c, -base));
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) l += pf[e] + pf[e + 1];
+                for (int e = 0; e < 8; e += 2) sum += pf[e] + pf[e + 1];
                 uint4 pw[3];
                 at_split8(pf, pw);
-                bf16x8 pb[3];
 #pragma unroll
-                for (int i = 0; i < 3; ++i) pb[i] = __builtin_bit_cast(bf16x8, pw[i]);
+                for (int i = 0; i < 3; ++i) {
+                    // formed here, between the products, and not where the outputs take them
+                    asm volatile("" : "+v"(pw[i].x), "+v"(pw[i].y), "+v"(pw[i].z), "+v"(pw[i].w));
+                    p[st][i] = __builtin_bit_cast(bf16x8, pw[i]);
+                }
+            }
+            l = l * f + sum;
+        };
+        auto rescale = [&]() {
+            if (ballot(f != 1.0f)) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
+            }
+        };
+        auto outputs = [&](int kb, const bf16x8 (&p)[2][3]) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     bf16x8 vf[3];
@@ -727,9 +739,25 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
                                        __builtin_bit_cast(uint2, v[1]).x, __builtin_bit_cast(uint2, v[1]).y);
                         vf[i] = __builtin_bit_cast(bf16x8, vw);
                     }
-                    oacc[d] = at_mfma6(vf, pb, oacc[d]);
+                    oacc[d] = at_mfma6(vf, p[st], oacc[d]);
                 }
-            }
+        };
+        scores(0);
+        drop(0);
+        if constexpr (NB == 2) {
+            bf16x8 pb1[2][3];
+            scores(1);
+            weights(0, pb);
+            rescale();
+            drop(1);
+            outputs(0, pb);
+            weights(1, pb1);
+            rescale();
+            outputs(1, pb1);
+        } else {
+            weights(0, pb);
+            rescale();
+            outputs(0, pb);
         }
         cur = nxt;
     }
