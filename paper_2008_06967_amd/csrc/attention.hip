@@ -1,4 +1,25 @@
-// Cross attention to another set of points.
+// Cross attention to another set of points: o_i = sum_j p_ij v_j / sum_j p_ij,
+// p_ij = exp(s_ij - m_i), s_ij = scale q_i . k_j.
+//
+// One pass over the sources with a running reference m_i and sum: where a
+// later score passes m_i by 8 (in powers of two) what was summed is scaled
+// down, otherwise m_i stays, so that the weights are at most 256 and most
+// tiles rescale nothing.  The queries of all heads that share a source head
+// are rows of one product (row = point x heads of the group + head), so K and
+// V are read once for them.
+//
+//   attention_bf16_kernel  bf16 on the matrix cores
+//   attention_f32_kernel   fp32 operands in three bf16 parts, many rows
+//   attention_f32_few_kernel  fp32 on the fp32 instruction, few rows
+//   attention_join_kernel  joins the parts of calls that split the sources
+//
+// Bounds.  Many rows: 4 D operations a pair on the matrix cores and the
+// weights on the vector units, which do not overlap whole.  4 x 16384 queries
+// over 4096 sources, 8 heads on 2, bf16: 1.10 ms, 1000 TFLOP/s at 128 channels
+// (matrix cores busy 46 %, 6.6 vector instructions counted a weight), 584 us,
+// 940 at 64 (41 %, 4.9), 396 us, 694 at 32; a large bf16 library product
+// reaches 1400.  Few rows: one read of K and V (8 x 1 query over 16384 sources,
+// 8 heads of 128: 188 us, 5.7 TB/s in fp32; 105 us, 5.1 TB/s in bf16).
 #include <algorithm>
 #include <cmath>
 
@@ -193,7 +214,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
     }
     const int tiles = (int)((end - begin + KT - 1) / KT);
 
-    // scores are compared and exponentiated in units of 1 / log2(e); a negative scale turns the queries around
+    // scores are exponentiated as powers of two; a negative scale turns the queries around
     const float c0 = a.scale * 1.44269504088896340736f;
     const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
     const uint32_t qflip = c0 < 0.0f ? 0x80008000u : 0u;
@@ -509,7 +530,9 @@ __device__ __forceinline__ f32x16 at_mfma6(const bf16x8 (&a)[3], const bf16x8 (&
 // matrix instructions a product: 419 TFLOP/s at most instead of the fp32
 // instruction's 157.  K and V are split once a tile, on their way to LDS (the
 // next tile's rows wait in registers); Q once, the weights where they form.
-// Four waves with 32 rows of their own.
+// Four waves with 32 rows of their own.  4 x 4096 queries over 1024 sources, 8
+// heads of 64: 185 us, 185 TFLOP/s, matrix cores busy 50 %; of 128: 457 us, 150,
+// busy 35 %, one wave a SIMD.
 template <int DB>
 struct AtF32 {
     static constexpr int KT = DB > 2 ? 32 : 64;                         // sources of a tile

@@ -1,4 +1,17 @@
-// Products in 8-bit integers with a scale for each row and output channel.
+// Products in 8-bit integers with a scale for each row and output channel:
+// y = (float(sum_c q_c w_c) s_row) s_channel + b, the sum exact in 32 bits.
+//
+// Float rows are first brought to 8 bits (quantize_i8_kernel), or, where at
+// most 16 rows of at most 2048 columns come, in the product's registers.
+//
+// Measured.  The large product (16384 x 4096 -> 4096, 8-bit rows): 269 us, 2040
+// TOP/s, where the library's int8 product without scales takes 244 us, 2250;
+// at 8192 x 8192 -> 8192 2270 against 2480.  The matrix cores are busy 49 % of
+// it and L2 serves 2.1 GB of tiles at 8 TB/s, so neither alone bounds it; what
+// takes the rest was not isolated.  16368 x 320 -> 256 from fp32: 16 us for the
+// 7 of its bytes, two launches and the 8-bit rows' round trip.  Few rows: the
+// latency of one chain of loads (13 x 1024 -> 512: 2.9 us from 8-bit rows, 6.1
+// from fp32).
 #include <algorithm>
 
 #include "common.h"
@@ -70,7 +83,8 @@ __device__ __forceinline__ void qu_store(int8_t* q, const float (&f)[N], const Q
 // LPR lanes per row, 16 bytes of a row (of any alignment) at a time; the first
 // kQuKeep vectors of a lane stay in registers between the maximum and the
 // rounding, longer rows are read again.  Bound: one read of x and one write
-// of q.
+// of q (16384 x 4096 bf16: 45 us, 4.5 TB/s in a
+// trace; 32 us repeated on the same rows, which the caches then hold in part).
 template <typename T, int LPR>
 __global__ __launch_bounds__(kQuThreads) void quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows,
                                                                  int C, int8_t* __restrict__ q, int64_t ldq,
@@ -214,8 +228,10 @@ __device__ __forceinline__ void lin_out(const LinArgs& a, int64_t row, int ch, i
 // Y^T = W X^T on v_mfma_i32_32x32x32_i8: a lane's accumulators of a 32 x 32
 // block are four runs of 4 channels of its own row, which it scales and
 // writes.  Both operands are 16-byte pieces of rows as they lie, from tiles
-// of 128 columns that are loaded ahead, two in LDS.  WC x WR waves, each of BC
-// x BR blocks (channels x rows).
+// of 128 columns that are loaded ahead, two in LDS, and a step's operands are
+// read between the products of the step before (when that came in: 468 to
+// 282 us for 16384 x 4096 -> 4096).  WC x WR waves, each of BC x BR blocks
+// (channels x rows).
 template <typename TY, int WC, int WR, int BC, int BR>
 __global__ __launch_bounds__(64 * WC * WR, (WC * WR >= 8 ? 2 : 1)) void linear_i8_kernel(LinArgs a) {
     constexpr int kThreads = 64 * WC * WR;
