@@ -592,6 +592,14 @@ def _workspace(x: torch.Tensor, need: int, ws):
     return ws.data_ptr(), ws.numel(), ws
 
 
+def _apart(out: torch.Tensor, *inputs):
+    """out must not be one of the inputs: other workgroups may still read what one has written."""
+    p = out.data_ptr()
+    for t in inputs:
+        if t.data_ptr() == p and t.numel() and out.numel():
+            raise ValueError("out must not be an input")
+
+
 def _new(x: torch.Tensor, shape, dtype=None) -> torch.Tensor:
     """An uninitialised contiguous tensor on x's device, of x's type unless given."""
     return x.new_empty(shape, dtype=dtype)
@@ -634,7 +642,7 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
     """Group norm over each cloud's valid points with an activation ("none",
     "relu", "silu", "gelu").  x [B, N, C] float32 or bfloat16; gamma, beta
     [C] float32; lens [B] int32 (rows from lens[b] on are not read and come
-    out 0).  out: like x, or of the other type (see the C header)."""
+    out 0).  out: like x, or of the other type (see the C header); not x."""
     _require(x.dim() == 3, "x must be [B, N, C]")
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
@@ -651,6 +659,7 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
         _require(out.shape == x.shape and out.device == x.device, "out must have x's shape and device")
         dy = _dtype(out, "out")
         py, ldy = _ld(out, "out")
+        _apart(out, x)
     wp, wn, ws = _workspace(x, _entry("group_norm_workspace")(B, N, C, groups, dt), ws)
     _call(x, "group_norm", px, ldx, dt, B, N, C, groups, _ptr(lens), _ptr(gamma), _ptr(beta), eps, _ACTS[act], py, ldy,
           dy, wp, wn)
@@ -670,6 +679,7 @@ def quantize_int8(x: torch.Tensor, out: torch.Tensor | None = None, scale: torch
     else:
         _require(out.dtype == torch.int8 and out.shape == x.shape and out.device == x.device,
                  "out must be int8 of x's shape, on x's device")
+        _apart(out, x)
     if scale is None:
         scale = _new(x, lead, torch.float32)
     else:
@@ -766,6 +776,7 @@ def linear_int8(x: torch.Tensor, p: Int8Params, x_scale: torch.Tensor | None = N
         _require(out.shape == lead + (p.c_out,) and out.device == x.device and out_dtype in (None, out.dtype),
                  "out must be [..., C_out] of out_dtype on x's device")
         py, ldy = _ld(out, "out")
+        _apart(out, x)
     wp, wn, ws = _workspace(x, _entry("linear_i8_workspace")(rows, c_in, p.c_out, dt), ws)
     _call(x, "linear_i8", px, ldx, dt, _ptr(x_scale), rows, c_in, *p.abi, 1 if relu else 0, py, ldy,
           _dtype(out, "out"), wp, wn)
@@ -850,7 +861,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     layout transposed, the filled part of a longer buffer).  k_len [B] int32:
     sources from k_len[b] on are not valid; k_mask [B, Nk] bool: only the True
     ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
-    unless given.  out: like q (its strides may differ)."""
+    unless given.  out: like q (its strides may differ), not q, k or v."""
     qs, ks = q.shape, k.shape
     _require(len(qs) == 4 and len(ks) == 4 and v.shape == ks, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
     B, Nq, Hq, D = qs
@@ -875,6 +886,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     else:
         _require(out.shape == qs and out.dtype is qd and out.device == dev, "out must be like q")
         po = _strides(out, qs, "out")
+        _apart(out, q, k, v)
     wp, wn, ws = _workspace(q, _entry("cross_attention_workspace")(B, Nq, Nk, Hq, Hkv, D, dt), ws)
     _call(q, "cross_attention", *_strides(q, qs, "q"), *_strides(k, ks, "k"), *_strides(v, ks, "v"), dt, B, Nq, Nk,
           Hq, Hkv, D, scale, _ptr(k_len), _ptr(k_mask), mask_ld, *po, wp, wn)

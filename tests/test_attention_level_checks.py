@@ -91,3 +91,19 @@ def test_cross_attention_refusals():
                      ((T(2, 5, 8, 4).transpose(2, 3), k, k), {})):
         with pytest.raises(ValueError):
             ops.cross_attention(*args, **kw)
+
+
+def test_out_must_not_be_an_input():
+    x = torch.zeros(2, 8, 16)
+    with pytest.raises(ValueError, match="out must not be an input"):
+        ops.group_norm(x, 4, out=x)
+    with pytest.raises(ValueError, match="out must not be an input"):
+        ops.group_norm(x[:, :, :8], 4, out=x[:, :, :8])
+    q = torch.zeros(1, 8, 2, 16)
+    k, v = torch.zeros(1, 8, 2, 16), torch.zeros(1, 8, 2, 16)
+    for o in (q, k, v):
+        with pytest.raises(ValueError, match="out must not be an input"):
+            ops.cross_attention(q, k, v, out=o)
+    # other columns of one buffer are apart: the call goes on to the device check
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        ops.group_norm(x[..., :8], 4, out=x[..., 8:])
