@@ -646,8 +646,9 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  * h reads source head h / (Hq / Hkv).  A query without any valid source (or
  * whose every score is -infinity) gives 0; k and v rows that are not valid
  * may hold anything, infinities and NaN included.  Maximum, sum and output
- * are accumulated in fp32; the bf16 form rounds the weights p to bf16 before
- * their product with v, the fp32 form keeps fp32 precision throughout.
+ * are accumulated in fp32; the bf16 form takes the weights p to their product
+ * with v in 16 bits of mantissa for few rows and rounded to bf16 for many,
+ * the fp32 form keeps fp32 precision throughout.
  *   q [B, Nq, Hq, D], k and v [B, Nk, Hkv, D], o [B, Nq, Hq, D], all of dtype
  *         (F32 or BF16), each with strides in elements: *_bs between clouds,
  *         *_ld between points, *_hs between heads; channels contiguous.  So

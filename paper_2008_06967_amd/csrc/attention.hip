@@ -181,6 +181,15 @@ __device__ __forceinline__ void at_write_part(const AttnArgs& a, int64_t pr, con
 // waves share the tiles of K and V: of 64 sources where each has rows of its
 // own, of 128, one block of 32 for each wave, where they share 32 rows (KS).
 // GEN: rows of any width and alignment, staged by elements.
+//
+// Where the waves share rows the weights are kept in two bf16 parts, 2^-16 of
+// each, and V is multiplied by both: such calls wait for memory or for their
+// few tiles (8 x 1 query over 16384 sources of 128 channels 105 us either way,
+// 1 x 1024 over 1024 of 64 10.8 -> 11.9).  With rows of their own they are
+// rounded to bf16, 2^-8 of each, whose errors average out over a row's sources
+// to about the output's own rounding: a second part costs what it adds to the
+// matrix cores and the vector units (4 x 16384 over 4096, 8 heads on 2: 1120 ->
+// 1530 us at 128 channels, 591 -> 877 at 64).
 template <int DB, int QB, bool KS, bool GEN>
 __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs a) {
     constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;       // 16-byte chunks of a row in LDS
@@ -359,7 +368,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
             }
         }
         // weights: the reference m of a query moves when its maximum passes it by 8 (a factor of 256)
-        uint32_t pk[QB][NB][8];
+        uint32_t pk[QB][NB][8], pl[QB][NB][8];           // pl: what the rounding left over (KS)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             float mx = -INFINITY;
@@ -388,9 +397,15 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
                     // the sum takes the rounded weights, as the product with V does
                     const float p0 = at_exp2(fmaf(s[qb][kb][r], c, -base));
                     const float p1 = at_exp2(fmaf(s[qb][kb][r + 1], c, -base));
-                    pk[qb][kb][r / 2] = at_pack(p0, p1);
-                    l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[qb][kb][r / 2]), ones, l[qb],
-                                                            false);
+                    const uint32_t hi = at_pack(p0, p1);
+                    pk[qb][kb][r / 2] = hi;
+                    l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, hi), ones, l[qb], false);
+                    if constexpr (KS) {
+                        const uint32_t lo =
+                            at_pack(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u));
+                        pl[qb][kb][r / 2] = lo;
+                        l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, lo), ones, l[qb], false);
+                    }
                 }
         }
         // outputs
@@ -414,6 +429,12 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
                     const bf16x8 vf = __builtin_bit_cast(bf16x8, vw);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) {
+                        if constexpr (KS) {
+                            const uint4 lw = make_uint4(pl[qb][kb][4 * st], pl[qb][kb][4 * st + 1],
+                                                        pl[qb][kb][4 * st + 2], pl[qb][kb][4 * st + 3]);
+                            oacc[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, lw),
+                                                                                  oacc[qb][d], 0, 0, 0);
+                        }
                         const uint4 pw = make_uint4(pk[qb][kb][4 * st], pk[qb][kb][4 * st + 1], pk[qb][kb][4 * st + 2],
                                                     pk[qb][kb][4 * st + 3]);
                         oacc[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pw),

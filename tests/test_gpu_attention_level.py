@@ -713,3 +713,19 @@ def test_offsets_past_32_bits(gpu):
     out = ops.cross_attention(qs, tail[:20].view(1, 20, 1, 64), tail[:20].view(1, 20, 1, 64))
     ref, bound = _ref_and_bound(tail.view(1, 300, 1, 64), tail[:20].view(1, 20, 1, 64), tail[:20].view(1, 20, 1, 64))
     within(out[:, -300:], ref, bound)
+
+
+# ---------------------------------------------------------------------------
+# the weights' precision
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,Nq,Nk,Hq,Hkv,D", [(2, 1, 50, 8, 2, 64), (1, 7, 2048, 4, 2, 128), (1, 300, 77, 2, 1, 32),
+                                              (1, 40, 1000, 2, 2, 90)])
+def test_attention_few_rows_keep_their_weights(gpu, B, Nq, Nk, Hq, Hkv, D):
+    """bf16 rows that share a workgroup: the weights' two bf16 parts leave out
+    2^-16 of each (a half step of a half step), the output is rounded once."""
+    g = gen(Nq + Nk)
+    q, k, v = (randn(g, B, n, h, D, dtype=H) for n, h in ((Nq, Hq), (Nk, Hkv), (Nk, Hkv)))
+    o, size, top = attention_ref(q, k, v)
+    e = 2 * ((D + 8) * U * top + 2.0 ** -21 + 128 * U) + 2 * 2.0 ** -16
+    within(ops.cross_attention(q, k, v), o, size * e + o.abs() * 2.0 ** -8 + 1e-30)
