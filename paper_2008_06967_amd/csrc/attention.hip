@@ -508,8 +508,8 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
 // ---------------------------------------------------------------------------
 
 // v = hi + mid + lo, each in bf16: 8 bits each of a float's 24, with nothing
-// left over -- of values from 2^-110 (below, the last parts may be denormal and
-// lost) to 3.38e38 (above, bf16 rounds to infinity).
+// left over -- of values from 2^-110 (below, what the last parts lose is at most
+// 2^-134) to 3.38e38 (above, and for infinities, the parts are no numbers).
 struct AtSplit {
     uint32_t hi, mid, lo;            // of two values
 };
@@ -554,86 +554,289 @@ __device__ __forceinline__ f32x16 at_mfma6(const bf16x8 (&a)[3], const bf16x8 (&
 // Four waves with 32 rows of their own.  4 x 4096 queries over 1024 sources, 8
 // heads of 64: 185 us, 185 TFLOP/s, matrix cores busy 50 %; of 128: 457 us, 150,
 // busy 35 %, one wave a SIMD.
+//
+// Values that the parts do not hold show in the results.  An infinity or a huge
+// value in k, or products past fp32's range with parts of either sign, give NaN
+// scores and sums; in v infinite or NaN outputs; and where v is so small that
+// 2^-134 counts, so are outputs.  A workgroup that finds such a result (from a
+// NaN of its inputs too), or a query outside [2^-102, 2^60] and 0, or a scale
+// that would show the small parts of k, goes over its tiles again with the fp32
+// instruction, for those queries alone.  (Testing every tile's values as they
+// are split instead took 7 to 17 % of the time.)
+constexpr float kAtLargeQ = 0x1p60f, kAtSmallQ = 0x1p-102f, kAtSmallOut = 0x1p-108f, kAtMaxScale = 0x1p20f;
+
 template <int DB>
 struct AtF32 {
     static constexpr int KT = DB > 2 ? 32 : 64;                         // sources of a tile
     static constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;           // 16-byte chunks of a row of one part
     static constexpr int kPart = KT * CH * 16;                          // bytes of one part of a tile
     static constexpr int kUnits = KT * CH / kAtThreads;                 // chunks of K (and of V) a thread stages
-    static constexpr int kLds = 6 * kPart;
+    static constexpr int kRow = 8 * CH + 4;                             // floats of a row that is not split
+    static constexpr int kFlags = 6 * kPart;                            // the waves' flags
+    static constexpr int kLds = kFlags + 16;
+    static_assert(2 * KT * kRow * 4 <= kFlags, "K and V in fp32 fit the parts' place");
 };
 
+// A workgroup's place: cloud, source head, part of the sources, query rows.
+struct AtPlace {
+    int64_t pair, b, begin, end;
+    int split, row0, kvh, g, tiles;
+    const uint8_t* mask;
+    __device__ __forceinline__ AtPlace(const AttnArgs& a, int64_t lb, int kt, int rows) {
+        split = (int)(lb % a.splits);
+        const int64_t rest = lb / a.splits;
+        row0 = (int)(rest % a.row_tiles) * rows;
+        pair = rest / a.row_tiles;
+        b = pair / a.Hkv;
+        kvh = (int)(pair - b * a.Hkv);
+        g = a.Hq / a.Hkv;
+        mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
+        begin = 0;
+        end = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
+        if (a.splits > 1) {
+            const int64_t per = ((end + a.splits - 1) / a.splits + kt - 1) / kt * kt;
+            begin = min(end, split * per);
+            end = min(end, begin + per);
+        }
+        tiles = (int)((end - begin + kt - 1) / kt);
+    }
+};
+
+// Eight channels from d0 on, zeros past D; without GEN D is a multiple of 4.
+template <bool GEN>
+__device__ __forceinline__ void at_read8(const AttnArgs& a, const float* p, int d0, bool ok, float (&f)[8]) {
+    if constexpr (GEN) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = ok && d0 + e < a.D ? p[d0 + e] : 0.0f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (ok && d0 + e < a.D) v = *reinterpret_cast<const float4*>(p + d0 + e);
+            f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
+        }
+    }
+}
+
+// A wave's 32 queries in fp32: running reference and sums, the scores' factor c
+// (of a power of two), the queries' factor (a negative scale turns them around,
+// a scale of 0 clears them).
+template <int DB>
+struct AtRows {
+    f32x16 oacc[DB];
+    float m, l, c, qmul;
+    __device__ __forceinline__ explicit AtRows(const AttnArgs& a) : m(-INFINITY), l(0.0f) {
+        const float c0 = a.scale * 1.44269504088896340736f;
+        c = c0 == 0.0f ? 1.0f : fabsf(c0);
+        qmul = c0 == 0.0f ? 0.0f : c0 < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
+    }
+    // sources of a block of 32 that are not valid
+    static __device__ __forceinline__ void drop(f32x16& s, uint32_t w32, int half) {
+        if (w32 != 0xffffffffu) {
+            const uint32_t w = w32 >> (4 * half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = (w >> (8 * (r / 4) + r % 4)) & 1 ? s[r] : -INFINITY;
+        }
+    }
+    // The reference m moves when a block's maximum passes it by 8; gives the factor of what was summed before.
+    __device__ __forceinline__ float advance(const f32x16& s) {
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        float lo;
+        const float hi = at_other_half(mx, lo);
+        mx = fmaxf(lo, hi) * c;
+        const float mn = mx > m + 8.0f ? mx : m;
+        const float f = mn == m ? 1.0f : at_exp2(m - mn);
+        m = mn;
+        return f;
+    }
+    __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }
+    __device__ __forceinline__ void rescale(float f) {
+        if (ballot(f != 1.0f)) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
+        }
+    }
+    // the two lanes of a query join their sums of weights
+    __device__ __forceinline__ void join_halves() {
+        float lo;
+        const float hi = at_other_half(l, lo);
+        l = lo + hi;
+    }
+    // a row without a weight is 0, whatever its sums hold
+    template <bool GEN>
+    __device__ __forceinline__ void write(const AttnArgs& a, const AtPlace& p, int row, int half) const {
+        if (row >= a.rows) return;
+        if (a.splits > 1) {
+            at_write_part<DB>(a, (p.pair * a.splits + p.split) * a.rows + row, oacc, m, l, half);
+            return;
+        }
+        const bool none = l == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / l;
+        const int n = row / p.g, h = p.kvh * p.g + (row - n * p.g);
+        float* op = static_cast<float*>(a.o) + p.b * a.ob + n * a.ol + h * a.oh;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int d0 = 32 * d + 2 * r + 4 * half;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = none ? 0.0f : oacc[d][r + e] * inv;
+                if constexpr (GEN) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (d0 + e < a.D) op[d0 + e] = v[e];
+                } else if (d0 < a.D) {
+                    *reinterpret_cast<float4*>(op + d0) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+    }
+};
+
+// A wave's queries in `again` on v_mfma_f32_32x32x2_f32, which takes any value:
+// a lane supplies row or column lane % 32 and k = lane / 32.  Scores: channels
+// 8 i + 4 (lane / 32) + e are step (i, e).  Outputs: step r takes the sources of
+// the lane's own weights.  Block, thread and arguments pass through an empty asm, so
+// that the kernel before it keeps none of this in registers (with it 4 to 8 %
+// slower).
 template <int DB, bool GEN>
-__global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_kernel(AttnArgs a) {
+__device__ __forceinline__ void attention_f32_plain(int block, int tid, uint32_t again, char* lds) {
+    using P = AtF32<DB>;
+    constexpr int CH = P::CH, KT = P::KT;
+    static_assert(sizeof(AttnArgs) % 8 == 0, "whole words");
+    struct Words {
+        uint64_t w[sizeof(AttnArgs) / 8];
+    } words;
+    auto* args = (__attribute__((address_space(4))) const uint64_t*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(block), "+v"(tid), "+s"(args));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(AttnArgs) / 8); ++i) words.w[i] = args[i];
+    const AttnArgs a = __builtin_bit_cast(AttnArgs, words);
+    const AtPlace p(a, (int64_t)(block & 7) * a.per_xcd + (block >> 3), KT, 128);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const float* __restrict__ kp = static_cast<const float*>(a.k) + p.b * a.kb + p.kvh * a.kh;
+    const float* __restrict__ vp = static_cast<const float*>(a.v) + p.b * a.vb + p.kvh * a.vh;
+    const int row = p.row0 + wave * 32 + col, rc = min(row, a.rows - 1), n = rc / p.g, h = p.kvh * p.g + (rc - n * p.g);
+    const float* qp = static_cast<const float*>(a.q) + p.b * a.qb + n * a.ql + h * a.qh;
+    float* pk = reinterpret_cast<float*>(lds);
+    float* pv = pk + KT * P::kRow;
+    AtRows<DB> o(a);
+#pragma unroll 1
+    for (int t = 0; t < p.tiles; ++t) {
+        const int64_t j0 = p.begin + (int64_t)t * KT;
+        uint64_t bits = at_count_bits(j0, p.end);
+        if (p.mask) bits &= ballot(j0 + lane < p.end && p.mask[j0 + lane]);
+        __syncthreads();             // the tile before has been read
+#pragma unroll 1
+        for (int i = 0; i < P::kUnits; ++i) {
+            const int u = i * kAtThreads + tid, r = u / CH, ch = u % CH;
+            const bool ok = (bits >> r) & 1;
+            float x[8], y[8];
+            at_read8<GEN>(a, kp + (j0 + r) * a.kl, 8 * ch, ok, x);
+            at_read8<GEN>(a, vp + (j0 + r) * a.vl, 8 * ch, ok, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                pk[r * P::kRow + 8 * ch + e] = x[e];
+                pv[r * P::kRow + 8 * ch + e] = y[e];
+            }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int kb = 0; kb < KT / 32; ++kb) {
+            f32x16 s;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll 1
+            for (int i = 0; i < 4 * DB; ++i) {
+                float q[8];
+                at_read8<GEN>(a, qp, 8 * i, o.qmul != 0.0f, q);
+                const float4 k = *reinterpret_cast<const float4*>(pk + (32 * kb + col) * P::kRow + 8 * i + 4 * half);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, (half ? q[4] : q[0]) * o.qmul, s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, (half ? q[5] : q[1]) * o.qmul, s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, (half ? q[6] : q[2]) * o.qmul, s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, (half ? q[7] : q[3]) * o.qmul, s, 0, 0, 0);
+            }
+            AtRows<DB>::drop(s, (uint32_t)(bits >> (32 * kb)), half);
+            const float f = o.advance(s), base = o.base();
+            o.rescale(f);
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = at_exp2(fmaf(s[r], o.c, -base));
+                sum += s[r];
+            }
+            o.l = o.l * f + sum;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float* v = pv + (32 * kb + 8 * (r / 4) + 4 * half + r % 4) * P::kRow + col;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    o.oacc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[32 * d], s[r], o.oacc[d], 0, 0, 0);
+            }
+        }
+    }
+    o.join_halves();
+    if ((again >> col) & 1) o.template write<GEN>(a, p, row, half);
+}
+
+template <int DB, bool GEN>
+__global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : DB == 2 ? 2 : 3)) void attention_f32_kernel(AttnArgs a) {
     using P = AtF32<DB>;
     constexpr int CH = P::CH, KT = P::KT, NB = KT / 32;
-    extern __shared__ __align__(16) char lds[];              // K's three parts, then V's
+    extern __shared__ __align__(16) char lds[];              // K's three parts, then V's; the waves' flags
 
     const int64_t lb = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
     if (lb >= a.blocks) return;
-    const int split = (int)(lb % a.splits);
-    const int64_t rest = lb / a.splits;
-    const int tile0 = (int)(rest % a.row_tiles);
-    const int64_t pair = rest / a.row_tiles;
-    const int64_t b = pair / a.Hkv;
-    const int kvh = (int)(pair - b * a.Hkv);
-    const int g = a.Hq / a.Hkv;
+    const AtPlace p(a, lb, KT, 128);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int half = lane >> 5, col = lane & 31;
 
-    const float* __restrict__ kp = static_cast<const float*>(a.k) + b * a.kb + kvh * a.kh;
-    const float* __restrict__ vp = static_cast<const float*>(a.v) + b * a.vb + kvh * a.vh;
-    const uint8_t* __restrict__ mask = a.k_mask ? a.k_mask + b * a.mask_ld : nullptr;
-    int64_t end = a.k_len ? min(max((int64_t)a.k_len[b], (int64_t)0), a.Nk) : a.Nk;
-    int64_t begin = 0;
-    if (a.splits > 1) {
-        const int64_t per = ((end + a.splits - 1) / a.splits + KT - 1) / KT * KT;
-        begin = min(end, split * per);
-        end = min(end, begin + per);
-    }
-    const int tiles = (int)((end - begin + KT - 1) / KT);
-
-    const float c0 = a.scale * 1.44269504088896340736f;
-    const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
-    const float qmul = c0 == 0.0f ? 0.0f : c0 < 0.0f ? -1.0f : 1.0f;
-
-    auto read8 = [&](const float* p, int d0, bool ok, float (&f)[8]) {
-        if constexpr (GEN) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = ok && d0 + e < a.D ? p[d0 + e] : 0.0f;
-        } else {                     // D is a multiple of 4
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (ok && d0 + e < a.D) v = *reinterpret_cast<const float4*>(p + d0 + e);
-                f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
-            }
-        }
-    };
+    const float* __restrict__ kp = static_cast<const float*>(a.k) + p.b * a.kb + p.kvh * a.kh;
+    const float* __restrict__ vp = static_cast<const float*>(a.v) + p.b * a.vb + p.kvh * a.vh;
+    const int64_t begin = p.begin, end = p.end;
+    const int tiles = p.tiles;
+    AtRows<DB> o(a);
+    const float c = o.c;
 
     // the wave's queries: operand B, channel 16 s + 8 half + e
-    const int row = tile0 * 128 + wave * 32 + col;
+    const int row = p.row0 + wave * 32 + col;
     bf16x8 qf[2 * DB][3];
+    float qtop = 0.0f;
+    uint32_t qlow = ~0u;             // of magnitudes that are not 0: twice their bits, less 1
     {
-        const int r = min(row, a.rows - 1), n = r / g, h = kvh * g + (r - n * g);
-        const float* qp = static_cast<const float*>(a.q) + b * a.qb + n * a.ql + h * a.qh;
+        const int r = min(row, a.rows - 1), n = r / p.g, h = p.kvh * p.g + (r - n * p.g);
+        const float* qp = static_cast<const float*>(a.q) + p.b * a.qb + n * a.ql + h * a.qh;
 #pragma unroll
         for (int s = 0; s < 2 * DB; ++s) {
             float f[8];
             uint4 w[3];
-            read8(qp, 16 * s + 8 * half, true, f);
+            at_read8<GEN>(a, qp, 16 * s + 8 * half, o.qmul != 0.0f, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = qmul == 0.0f ? 0.0f : f[e] * qmul;
+            for (int e = 0; e < 8; ++e) {
+                f[e] *= o.qmul;
+                qtop = fmaxf(qtop, fabsf(f[e]));
+                qlow = min(qlow, (__float_as_uint(f[e]) << 1) - 1u);
+            }
             at_split8(f, w);
 #pragma unroll
             for (int i = 0; i < 3; ++i) qf[s][i] = __builtin_bit_cast(bf16x8, w[i]);
         }
     }
+    const uint64_t q_lanes = ballot(c > kAtMaxScale || qtop > kAtLargeQ ||
+                                    qlow < (__builtin_bit_cast(uint32_t, kAtSmallQ) << 1) - 1u);
 
     auto valid_bits = [&](int t) {
         const int64_t j = begin + (int64_t)t * KT;
         uint64_t bits = at_count_bits(j, end);
-        if (mask) bits &= ballot(j + lane < end && mask[j + lane]);
+        if (p.mask) bits &= ballot(j + lane < end && p.mask[j + lane]);
         return bits;
     };
     float kr[P::kUnits][8], vr[P::kUnits][8];
@@ -641,10 +844,10 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
         const int64_t j0 = begin + (int64_t)t * KT;
 #pragma unroll
         for (int i = 0; i < P::kUnits; ++i) {
-            const int p = i * kAtThreads + tid, r = p / CH, ch = (p % CH) ^ at_swz<CH>(r);
+            const int u = i * kAtThreads + tid, r = u / CH, ch = (u % CH) ^ at_swz<CH>(r);
             const bool ok = (bits >> r) & 1;
-            read8(kp + (j0 + r) * a.kl, 8 * ch, ok, kr[i]);
-            read8(vp + (j0 + r) * a.vl, 8 * ch, ok, vr[i]);
+            at_read8<GEN>(a, kp + (j0 + r) * a.kl, 8 * ch, ok, kr[i]);
+            at_read8<GEN>(a, vp + (j0 + r) * a.vl, 8 * ch, ok, vr[i]);
         }
     };
     auto store = [&]() {
@@ -661,13 +864,6 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
             }
         }
     };
-
-    f32x16 oacc[DB];
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
 
     const int swk = at_swz<CH>(col);
     const int vi = lane & 15, vg = (lane >> 4) & 1;
@@ -713,27 +909,10 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
                 s[kb] = at_mfma6(kf[st & 1], qf[st], s[kb]);
             }
         };
-        auto drop = [&](int kb) {            // sources that are not valid
-            const uint32_t w32 = (uint32_t)(cur >> (32 * kb));
-            if (w32 != 0xffffffffu) {
-                const uint32_t w = w32 >> (4 * half);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kb][r] = (w >> (8 * (r / 4) + r % 4)) & 1 ? s[kb][r] : -INFINITY;
-            }
-        };
-        // weights in three parts, and the factor f of what was summed before: a query's reference m moves when its
-        // maximum passes it by 8
+        // weights in three parts, and the factor f of what was summed before
         auto weights = [&](int kb, bf16x8 (&p)[2][3]) {
-            float mx = s[kb][0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-            float lo;
-            const float hi = at_other_half(mx, lo);
-            mx = fmaxf(lo, hi) * c;
-            const float mn = mx > m + 8.0f ? mx : m;
-            f = mn == m ? 1.0f : at_exp2(m - mn);
-            m = mn;
-            const float base = m == -INFINITY ? 0.0f : m;
+            f = o.advance(s[kb]);
+            const float base = o.base();
             float sum = 0.0f;
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
@@ -752,15 +931,7 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
                     p[st][i] = __builtin_bit_cast(bf16x8, pw[i]);
                 }
             }
-            l = l * f + sum;
-        };
-        auto rescale = [&]() {
-            if (ballot(f != 1.0f)) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
-            }
+            o.l = o.l * f + sum;
         };
         auto outputs = [&](int kb, const bf16x8 (&p)[2][3]) {
 #pragma unroll
@@ -783,56 +954,50 @@ __global__ __launch_bounds__(kAtThreads, (DB > 2 ? 1 : 2)) void attention_f32_ke
                                        __builtin_bit_cast(uint2, v[1]).x, __builtin_bit_cast(uint2, v[1]).y);
                         vf[i] = __builtin_bit_cast(bf16x8, vw);
                     }
-                    oacc[d] = at_mfma6(vf, p[st], oacc[d]);
+                    o.oacc[d] = at_mfma6(vf, p[st], o.oacc[d]);
                 }
         };
         scores(0);
-        drop(0);
+        o.drop(s[0], (uint32_t)cur, half);
         if constexpr (NB == 2) {
             bf16x8 pb1[2][3];
             scores(1);
             weights(0, pb);
-            rescale();
-            drop(1);
+            o.rescale(f);
+            o.drop(s[1], (uint32_t)(cur >> 32), half);
             outputs(0, pb);
             weights(1, pb1);
-            rescale();
+            o.rescale(f);
             outputs(1, pb1);
         } else {
             weights(0, pb);
-            rescale();
+            o.rescale(f);
             outputs(0, pb);
         }
         cur = nxt;
     }
 
-    {
-        float lo;
-        const float hi = at_other_half(l, lo);
-        l = lo + hi;
-    }
-    if (row >= a.rows) return;
-    if (a.splits > 1) {
-        at_write_part<DB>(a, (pair * a.splits + split) * a.rows + row, oacc, m, l, half);
-        return;
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int n = row / g, h = kvh * g + (row - n * g);
-    float* op = static_cast<float*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
+    o.join_halves();
+
+    // results that ask for the fp32 instruction: times 0 they are not 0, or they are small but not 0
+    float nan = o.l * 0.0f;
+    uint32_t low = ~0u;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int d0 = 32 * d + 2 * r + 4 * half;
-            if constexpr (GEN) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (d0 + e < a.D) op[d0 + e] = oacc[d][r + e] * inv;
-            } else if (d0 < a.D) {
-                *reinterpret_cast<float4*>(op + d0) = make_float4(oacc[d][r] * inv, oacc[d][r + 1] * inv,
-                                                                  oacc[d][r + 2] * inv, oacc[d][r + 3] * inv);
-            }
+        for (int r = 0; r < 16; ++r) {
+            nan = fmaf(o.oacc[d][r], 0.0f, nan);
+            low = min(low, (__float_as_uint(o.oacc[d][r]) << 1) - 1u);
         }
+    const uint64_t lanes =
+        q_lanes | ballot(nan != 0.0f || low < (__float_as_uint(o.l * kAtSmallOut) << 1) - 1u);
+    const uint32_t again = (uint32_t)lanes | (uint32_t)(lanes >> 32);        // of the wave's queries
+    if (lane == 0) reinterpret_cast<uint32_t*>(lds + P::kFlags)[wave] = again;
+    if (!((again >> col) & 1)) o.template write<GEN>(a, p, row, half);
+    __syncthreads();
+    const uint4 all = *reinterpret_cast<const uint4*>(lds + P::kFlags);
+    if (__builtin_amdgcn_readfirstlane(all.x | all.y | all.z | all.w))
+        attention_f32_plain<DB, GEN>(blockIdx.x, threadIdx.x, again, lds);
 }
 
 // Few rows in fp32: 16 RB query rows, the fp32 instruction, and K and V from

@@ -729,3 +729,61 @@ def test_attention_few_rows_keep_their_weights(gpu, B, Nq, Nk, Hq, Hkv, D):
     o, size, top = attention_ref(q, k, v)
     e = 2 * ((D + 8) * U * top + 2.0 ** -21 + 128 * U) + 2 * 2.0 ** -16
     within(ops.cross_attention(q, k, v), o, size * e + o.abs() * 2.0 ** -8 + 1e-30)
+
+
+# ---------------------------------------------------------------------------
+# values that the fp32 products' parts do not hold
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("Nq,Nk,D", [(2, 300, 64), (140, 300, 64), (300, 90, 32), (150, 700, 128), (130, 70, 90),
+                                     (1, 3000, 40), (129, 33, 31)])
+@pytest.mark.parametrize("what", ["k -inf", "k lowest", "score past fp32", "v large", "v tiny", "q large", "q rows"])
+def test_attention_any_values(gpu, dtype, Nq, Nk, D, what):
+    """Infinite, huge and tiny values in valid sources and queries, at any
+    number of rows: a source whose score is -infinity, or passes fp32's range
+    downwards, weighs 0, so the reference is the one without it."""
+    g = gen(Nq + Nk + D)
+    B, Hq, Hkv = 2, 2, 1
+    q, k, v = (randn(g, B, n, h, D, dtype=dtype) for n, h in ((Nq, Hq), (Nk, Hkv), (Nk, Hkv)))
+    gone = torch.rand((B, Nk), generator=g, device="cuda") < 0.1
+    gone[0, 40:] = False                            # the first cloud has them in its first tiles only
+    gone[:, 0], gone[:, 1] = True, False
+    c = D // 2
+    extra = 0.0
+    if what in ("k -inf", "k lowest"):
+        q[..., c] = q[..., c].abs() + 0.5
+        clean = k.clone()
+        k[..., c][gone] = -math.inf if what == "k -inf" else torch.finfo(dtype).min
+    elif what == "score past fp32":
+        q[..., c], k[..., c] = 0.0, 0.0
+        clean = (q.clone(), k.clone())
+        q[..., c] = 1.003e25
+        k[..., c][gone] = -1.003e25
+    elif what == "q large":                         # scores of the usual size from factors far from it
+        k = (k.float() * 2.0 ** -90).to(dtype)
+        q = (q.float() * 2.0 ** 90).to(dtype)
+        clean, gone = k, torch.zeros_like(gone)
+    elif what == "q rows":                          # one query's scores are -infinity for all but one source
+        clean, gone = k, torch.zeros_like(gone)
+        k[..., c] = k[..., c].abs() + 0.5
+        k[:, 1, :, c] = 0.0
+    else:
+        f = 1e28 if what == "v large" else 1e-38
+        v = (v.float() * f).to(dtype)
+        clean, gone = k, torch.zeros_like(gone)
+        # fp32's denormal step, 2^-149: a product and a sum for each source, and bf16's for the output
+        extra = 0.0 if f > 1 else (Nk * 2.0 ** -148 + (2.0 ** -133 if dtype == H else 0.0))
+    if what == "score past fp32":
+        ref, bound = _ref_and_bound(clean[0], clean[1], v, k_mask=~gone)
+    else:
+        ref, bound = _ref_and_bound(q, clean, v, k_mask=~gone)
+    if what == "q rows":
+        q[:, 0, :, c] = -math.inf                   # 0 x -inf is NaN: so that source is dropped instead
+        mask = torch.ones((B, Nk), dtype=torch.bool, device="cuda")
+        mask[:, 1] = False
+        ref, bound = _ref_and_bound(torch.where(torch.isinf(q), torch.zeros_like(q), q), k, v, k_mask=mask)
+        ref[:, 0], bound[:, 0] = 0.0, 0.0
+        within(ops.cross_attention(q, k, v, k_mask=mask), ref, bound)
+        return
+    within(ops.cross_attention(q, k, v), ref, bound + extra)
