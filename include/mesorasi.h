@@ -646,10 +646,10 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  * h reads source head h / (Hq / Hkv).  A query without any valid source (or
  * whose every score is -infinity) gives 0; k and v rows that are not valid
  * may hold anything, infinities and NaN included.  Maximum, sum and output
- * are accumulated in fp32; the bf16 form takes the weights p to their product
- * with v in 16 bits of mantissa for few rows and rounded to bf16 for many,
- * the fp32 form keeps fp32 precision throughout (v below fp32's normal range
- * may count as 0).  Scores past fp32's range are infinite: a source of score
+ * are accumulated in fp32.  The bf16 form takes the weights p to their product
+ * with v in 15 bits for few rows, rounded to bf16 for many; the fp32 form keeps
+ * fp32 precision throughout (v below fp32's normal range may count as 0).
+ * Scores past fp32's range are infinite: a source of score
  * -infinity weighs 0, one of +infinity or NaN makes its queries NaN.  The sums
  * of 256 |v| over a query's valid sources have to stay within fp32's range.
  *   q [B, Nq, Hq, D], k and v [B, Nk, Hkv, D], o [B, Nq, Hq, D], all of dtype

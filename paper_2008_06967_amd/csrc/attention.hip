@@ -182,10 +182,11 @@ __device__ __forceinline__ void at_write_part(const AttnArgs& a, int64_t pr, con
 // own, of 128, one block of 32 for each wave, where they share 32 rows (KS).
 // GEN: rows of any width and alignment, staged by elements.
 //
-// Where the waves share rows the weights are kept in two bf16 parts, 2^-16 of
+// Where the waves share rows the weights are kept in two bf16 parts, to 2^-15 of
 // each, and V is multiplied by both: such calls wait for memory or for their
 // few tiles (8 x 1 query over 16384 sources of 128 channels 105 us either way,
-// 1 x 1024 over 1024 of 64 10.8 -> 11.9).  With rows of their own they are
+// 1 x 1024 over 1024 of 64 10.8 -> 12.4).  The first part is rounded down and
+// the second above 0, so that an infinite v meets no 0 and no other sign.  With rows of their own they are
 // rounded to bf16, 2^-8 of each, whose errors average out over a row's sources
 // to about the output's own rounding: a second part costs what it adds to the
 // matrix cores and the vector units (4 x 16384 over 4096, 8 heads on 2: 1120 ->
@@ -397,12 +398,14 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
                     // the sum takes the rounded weights, as the product with V does
                     const float p0 = at_exp2(fmaf(s[qb][kb][r], c, -base));
                     const float p1 = at_exp2(fmaf(s[qb][kb][r + 1], c, -base));
-                    const uint32_t hi = at_pack(p0, p1);
+                    const uint32_t b0 = __float_as_uint(p0) & 0xffff0000u, b1 = __float_as_uint(p1) & 0xffff0000u;
+                    const uint32_t hi = KS ? b0 >> 16 | b1 : at_pack(p0, p1);
                     pk[qb][kb][r / 2] = hi;
                     l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, hi), ones, l[qb], false);
                     if constexpr (KS) {
-                        const uint32_t lo =
-                            at_pack(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u));
+                        // p (1 + 2^-23) - hi
+                        const uint32_t lo = at_pack(fmaf(p0, 1.00000012f, -__uint_as_float(b0)),
+                                                    fmaf(p1, 1.00000012f, -__uint_as_float(b1)));
                         pl[qb][kb][r / 2] = lo;
                         l[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, lo), ones, l[qb], false);
                     }

@@ -722,12 +722,13 @@ def test_offsets_past_32_bits(gpu):
 @pytest.mark.parametrize("B,Nq,Nk,Hq,Hkv,D", [(2, 1, 50, 8, 2, 64), (1, 7, 2048, 4, 2, 128), (1, 300, 77, 2, 1, 32),
                                               (1, 40, 1000, 2, 2, 90)])
 def test_attention_few_rows_keep_their_weights(gpu, B, Nq, Nk, Hq, Hkv, D):
-    """bf16 rows that share a workgroup: the weights' two bf16 parts leave out
-    2^-16 of each (a half step of a half step), the output is rounded once."""
+    """bf16 rows that share a workgroup: the first of a weight's two bf16 parts is
+    rounded down and leaves 2^-7 of it at most, the second half a step of that,
+    2^-15; twice, for the sum of the weights; the output is rounded once."""
     g = gen(Nq + Nk)
     q, k, v = (randn(g, B, n, h, D, dtype=H) for n, h in ((Nq, Hq), (Nk, Hkv), (Nk, Hkv)))
     o, size, top = attention_ref(q, k, v)
-    e = 2 * ((D + 8) * U * top + 2.0 ** -21 + 128 * U) + 2 * 2.0 ** -16
+    e = 2 * ((D + 8) * U * top + 2.0 ** -21 + 128 * U) + 2 * 2.0 ** -15
     within(ops.cross_attention(q, k, v), o, size * e + o.abs() * 2.0 ** -8 + 1e-30)
 
 
@@ -787,3 +788,28 @@ def test_attention_any_values(gpu, dtype, Nq, Nk, D, what):
         within(ops.cross_attention(q, k, v, k_mask=mask), ref, bound)
         return
     within(ops.cross_attention(q, k, v), ref, bound + extra)
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("Nq", [3, 200])
+def test_attention_infinite_v_and_nan_sources(gpu, dtype, Nq):
+    """An infinity in v reaches its own channel with its sign; a NaN in a
+    valid source's v its own channel, in its k every query of the head."""
+    g = gen(31)
+    Nk, D = 120, 64
+    q, k, v = (randn(g, 2, n, h, D, dtype=dtype) for n, h in ((Nq, 4), (Nk, 2), (Nk, 2)))
+    ref, bound = _ref_and_bound(q, k, v)
+    v[0, 7, 0, 3], v[1, 100, 1, 60] = math.inf, -math.inf
+    v[1, 5, 0, 9] = math.nan
+    k[1, 110, 1, 1] = math.nan
+    ref[0, :, :2, 3], ref[1, :, :2, 9], ref[1, :, 2:] = math.inf, math.nan, math.nan
+    within(ops.cross_attention(q, k, v), ref, bound)
+
+
+@pytest.mark.parametrize("Nq,Nk", [(3, 200), (150, 300)])
+def test_attention_tiny_v(gpu, Nq, Nk):
+    """fp32 v of 1e-38 under equal weights: off by the sums' roundings and by
+    fp32's denormal steps, one for each source's product and sum."""
+    g = gen(32)
+    q, k = torch.zeros((2, Nq, 2, 64), device="cuda"), randn(g, 2, Nk, 2, 64)
+    v = randn(g, 2, Nk, 2, 64) * 1e-38
+    ref, bound = _ref_and_bound(q, k, v)
+    within(ops.cross_attention(q, k, v), ref, bound - 1e-30 + Nk * 2.0 ** -148)
