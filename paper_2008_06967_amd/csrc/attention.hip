@@ -131,13 +131,15 @@ __device__ __forceinline__ void at_join_waves(const AttnArgs& a, const float* sh
     T* op = static_cast<T*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
     const int64_t pr = (pair * a.splits + split) * a.rows + row;
     for (int d = tid / R; d < a.D; d += 64 * W / R) {
-        float v = 0.0f;
+        float v = 0.0f, part[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) v += mm[w] * sh[(w * Dp + d) * R + r];
+        for (int w = 0; w < W; ++w) part[w] = mm[w] * sh[(w * Dp + d) * R + r];
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += mm[w] == 0.0f ? 0.0f : part[w];
         if (a.splits > 1) {
             a.part[pr * a.Dp + d] = v;
         } else {
-            v *= inv;
+            v = L == 0.0f ? 0.0f : v * inv;      // 0 without a weight, whatever the sums hold
             if constexpr (sizeof(T) == 4)
                 op[d] = v;
             else
@@ -484,7 +486,8 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
                 at_write_part<DB>(a, (pair * a.splits + split) * a.rows + row, oacc[qb], m[qb], l[qb], half);
                 continue;
             }
-            const float inv = l[qb] == 0.0f ? 0.0f : 1.0f / l[qb];
+            const bool none = l[qb] == 0.0f;         // 0 then, whatever the sums hold
+            const float inv = none ? 0.0f : 1.0f / l[qb];
             const int n = row / g, h = kvh * g + (row - n * g);
             uint16_t* op = static_cast<uint16_t*>(a.o) + b * a.ob + n * a.ol + h * a.oh;
 #pragma unroll
@@ -492,14 +495,15 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int d0 = 32 * d + 2 * r + 4 * half;
-                    const f32x16 v = oacc[qb][d];
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = none ? 0.0f : oacc[qb][d][r + e] * inv;
                     if constexpr (GEN) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (d0 + e < a.D) op[d0 + e] = f32_to_bf16_any(v[r + e] * inv);
+                            if (d0 + e < a.D) op[d0 + e] = f32_to_bf16_any(v[e]);
                     } else if (d0 < a.D) {
-                        *reinterpret_cast<uint2*>(op + d0) =
-                            make_uint2(at_pack(v[r] * inv, v[r + 1] * inv), at_pack(v[r + 2] * inv, v[r + 3] * inv));
+                        *reinterpret_cast<uint2*>(op + d0) = make_uint2(at_pack(v[0], v[1]), at_pack(v[2], v[3]));
                     }
                 }
         }

@@ -813,3 +813,18 @@ def test_attention_tiny_v(gpu, Nq, Nk):
     v = randn(g, 2, Nk, 2, 64) * 1e-38
     ref, bound = _ref_and_bound(q, k, v)
     within(ops.cross_attention(q, k, v), ref, bound - 1e-30 + Nk * 2.0 ** -148)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("Nq,Nk", [(2, 40), (2, 2000), (70, 130), (200, 90), (3000, 65)])
+def test_attention_rows_without_a_weight(gpu, dtype, Nq, Nk):
+    """Queries whose every score is -infinity give 0, whatever v holds."""
+    g = gen(33)
+    q, k, v = (randn(g, 2, n, h, 48, dtype=dtype) for n, h in ((Nq, 8), (Nk, 4), (Nk, 4)))
+    q[..., 3] = q[..., 3].abs() + 0.5
+    k[1, ..., 3] = -math.inf
+    v[1] = torch.tensor([math.inf, -math.inf, math.nan, 1.0], device="cuda").to(dtype).repeat(12)
+    ref, bound = _ref_and_bound(q[:1], k[:1], v[:1])
+    got = ops.cross_attention(q, k, v)
+    within(got[:1], ref, bound)
+    assert bool((got[1] == 0).all())
