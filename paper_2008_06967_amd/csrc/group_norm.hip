@@ -1,10 +1,11 @@
 // Group normalisation with an activation, channels last.
 //
 // Mean and variance are joined from parts, each (count, mean, sum of squared
-// differences to that mean), so that nothing cancels: a thread sums
-// differences to its own first value, parts join by differences of their
-// means, and means are kept relative to the group's first value, so that an
-// offset of the data costs no accuracy.  Parts are joined in a fixed order.
+// differences to that mean), so that nothing cancels.  A mean is a sum of two
+// floats, the second what the first's rounding leaves, and every join takes
+// differences to a first estimate of the mean and corrects it by their own mean:
+// so neither an offset of the data nor single values far from the others cost
+// the others accuracy, wherever they stand.  Parts are joined in a fixed order.
 //
 // Two forms.  Where the rows of a run of whole groups fit the registers of
 // one workgroup, it reads them once, and one launch does all.  Otherwise one
@@ -35,13 +36,18 @@ struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) GnVec {
     T e[N];
 };
 
+// Mean (hi + lo, hi the nearest float) and sum of squared differences to it.
+struct GnPart {
+    float hi, lo, m2;
+};
+
 struct GnArgs {
     const void* x;
     void* y;
     const int32_t* lens;
     const float* gamma;
     const float* beta;
-    float2* part;                    // [B, chunks, groups, pieces]: mean, sum of squared differences
+    GnPart* part;                    // [B, chunks, groups, pieces]
     int64_t ldx, ldy, B, N;
     int C, G, c;
     float eps;
@@ -118,9 +124,23 @@ __device__ __forceinline__ int gn_lanes(int groups, int parts) {
     return __builtin_amdgcn_readfirstlane(w);
 }
 
+// a + b as the nearest float and what it leaves (Knuth's two-sum).
+__device__ __forceinline__ void gn_two_sum(float a, float b, float& hi, float& lo) {
+    hi = a + b;
+    const float t = hi - a;
+    lo = (a - (hi - t)) + (b - t);
+}
+
+// v, or 0 where roundings left less; NaN stays.
+__device__ __forceinline__ float gn_positive(float v) { return v < 0.0f ? 0.0f : v; }
+
+__device__ __forceinline__ float gn_diff(const GnPart& a, const GnPart& b) { return (a.hi - b.hi) + (a.lo - b.lo); }
+
+// m's mean moved by d.
+__device__ __forceinline__ void gn_move(GnPart& m, float d) { gn_two_sum(m.hi, m.lo + d, m.hi, m.lo); }
+
 // The groups' parts in LDS, joined: part (s, e), e < per, of a group counts
-// n(s) values and is get(g, s, e) = (mean, sum of squares); put(g, n, mean,
-// m2) takes the result.
+// n(s) values and is get(g, s, e); put(g, part) takes the result.
 template <int THREADS, typename Count, typename Get, typename Put>
 __device__ __forceinline__ void gn_join(int groups, int slots, int per, Count n, Get get, Put put) {
     const int w = gn_lanes<THREADS>(groups, slots * per);
@@ -129,25 +149,31 @@ __device__ __forceinline__ void gn_join(int groups, int slots, int per, Count n,
     const int lw = __builtin_ctz(w), le = __builtin_ctz(we);
     const int lane = threadIdx.x & (w - 1), ws = w >> le, s0 = lane >> le, e0 = lane & (we - 1);
     for (int g = threadIdx.x >> lw; g < groups; g += THREADS >> lw) {
-        const float m0 = get(g, 0, 0).x;
+        GnPart m = get(g, 0, 0);
         float cnt = 0.0f, sum = 0.0f;
         for (int s = s0; s < slots; s += ws)
             for (int e = e0; e < per; e += we) {
                 const float k = n(s);
                 cnt += k;
-                sum += k * (get(g, s, e).x - m0);
+                sum += k * gn_diff(get(g, s, e), m);
             }
         cnt = lane_sum(cnt, w);
-        const float d = lane_sum(sum, w) / cnt;
+        gn_move(m, lane_sum(sum, w) / cnt);
         float m2 = 0.0f;
+        sum = 0.0f;
         for (int s = s0; s < slots; s += ws)
             for (int e = e0; e < per; e += we) {
-                const float2 v = get(g, s, e);
-                const float t = (v.x - m0) - d;
-                m2 += v.y + n(s) * t * t;
+                const GnPart v = get(g, s, e);
+                const float t = gn_diff(v, m), nt = n(s) * t;
+                sum += nt;
+                m2 += v.m2 + nt * t;
             }
+        sum = lane_sum(sum, w);
         m2 = lane_sum(m2, w);
-        if (lane == 0) put(g, cnt, m0 + d, m2);
+        const float d = sum / cnt;
+        gn_move(m, d);
+        m.m2 = gn_positive(m2 - sum * d);
+        if (lane == 0) put(g, m);
     }
 }
 
@@ -195,8 +221,8 @@ struct GnPlace {
     }
 };
 
-// A thread's channels: their groups, each group's first value (what its rows
-// are compared with), gamma and beta.
+// A thread's channels: their groups, gamma and beta, and what is taken from
+// their values (the group's first value, then its mean).
 template <int VEC>
 struct GnChannels {
     int grp[VEC];
@@ -205,6 +231,7 @@ struct GnChannels {
 
 template <typename TX, int VEC, typename P>
 __device__ __forceinline__ void gn_channels(const GnArgs& a, const P& p, GnChannels<VEC>& c) {
+    // the one-launch form's first estimate of a group's mean is taken from its first value on
     const TX* x0 = static_cast<const TX*>(a.x) + p.b * a.N * a.ldx + (int64_t)p.first * a.c;
     p.channel_groups(a, c.grp);
 #pragma unroll
@@ -230,31 +257,32 @@ __device__ __forceinline__ void gn_affine(const GnArgs& a, const P& p, GnChannel
         for (int k = 0; k < VEC; ++k) c.beta[k] = a.beta[ch + k];
 }
 
-// The thread's channels' parts (mean relative to its group's first value,
-// squares) to LDS: channels of one group join at once.
+// The thread's channels' parts to LDS: channels of one group join at once.
 template <int VEC>
-__device__ __forceinline__ void gn_put_parts(bool merged, float n, const float (&mean)[VEC], const float (&m2)[VEC],
-                                             float2* ent) {
+__device__ __forceinline__ void gn_put_parts(bool merged, float n, const GnPart (&c)[VEC], GnPart* ent) {
     if (!merged) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) ent[k] = make_float2(mean[k], m2[k]);
+        for (int k = 0; k < VEC; ++k) ent[k] = c[k];
         return;
     }
     float d = 0.0f, q = 0.0f;
 #pragma unroll
-    for (int k = 1; k < VEC; ++k) d += mean[k] - mean[0];
+    for (int k = 1; k < VEC; ++k) d += gn_diff(c[k], c[0]);
     d *= 1.0f / VEC;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-        const float t = (mean[k] - mean[0]) - d;
-        q += m2[k] + n * t * t;
+        const float t = gn_diff(c[k], c[0]) - d;
+        q += c[k].m2 + n * t * t;
     }
-    *ent = make_float2(mean[0] + d, q);
+    GnPart m = c[0];
+    gn_move(m, d);
+    m.m2 = q;
+    *ent = m;
 }
 
 template <typename TX, int VEC>
 __global__ __launch_bounds__(kGnThreads) void gn_parts_kernel(GnArgs a) {
-    __shared__ float2 ent[kGnThreads * VEC];
+    __shared__ GnPart ent[kGnThreads * VEC];
     int chunk;
     const int rest = a.by_chunks.div((int)blockIdx.x, chunk);
     const GnPlace<kGnThreads, VEC> p(a, rest);
@@ -262,70 +290,77 @@ __global__ __launch_bounds__(kGnThreads) void gn_parts_kernel(GnArgs a) {
     if (r0 >= r1) return;                        // no valid row: the join knows
     const int nrows = (int)(r1 - r0);
     const bool merged = a.pieces > 1 || a.c % VEC == 0;
-    GnChannels<VEC> c;
-    gn_channels<TX, VEC>(a, p, c);
     float sum[VEC] = {}, sq[VEC] = {}, f[VEC] = {};
+    GnPart part[VEC] = {};
     const int full = nrows / p.slots, tail = nrows - full * p.slots;      // rows of every slot, slots with one more
     const int mine = p.on ? full + (p.slot < tail) : 0;
     if (mine > 0) {
         const TX* xp = static_cast<const TX*>(a.x) + (p.b * a.N + r0 + p.slot) * a.ldx + p.ch0 + p.vec * VEC;
         const int64_t step = (int64_t)p.slots * a.ldx;
-        GnVec<TX, VEC> w = *reinterpret_cast<const GnVec<TX, VEC>*>(xp);
+        // The differences are taken to the median of a channel's first three values: to one far from the others they
+        // would all be rounded as coarsely as it, and so would their sum.
+        GnVec<TX, VEC> w[3];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) f[k] = gn_float(w.e[k]);
-#pragma unroll 4
-        for (int i = 1; i < mine; ++i) {
-            w = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + i * step);
+        for (int i = 0; i < 3; ++i) w[i] = *reinterpret_cast<const GnVec<TX, VEC>*>(xp + min(i, mine - 1) * step);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            f[k] = __builtin_amdgcn_fmed3f(gn_float(w[0].e[k]), gn_float(w[1].e[k]), gn_float(w[2].e[k]));
+        auto add = [&](const GnVec<TX, VEC>& v) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
-                const float d = gn_float(w.e[k]) - f[k];
+                const float d = gn_float(v.e[k]) - f[k];
                 sum[k] += d;
                 sq[k] = fmaf(d, d, sq[k]);
             }
-        }
+        };
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < mine) add(w[i]);
+#pragma unroll 4
+        for (int i = 3; i < mine; ++i) add(*reinterpret_cast<const GnVec<TX, VEC>*>(xp + i * step));
         const float n = (float)mine;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             const float d = sum[k] / n;
-            sq[k] -= sum[k] * d;
-            f[k] = (f[k] - c.ref[k]) + d;
+            gn_two_sum(f[k], d, part[k].hi, part[k].lo);
+            part[k].m2 = gn_positive(sq[k] - sum[k] * d);
         }
     }
     const int nv = (int)a.by_nv.d;
-    if (p.on) gn_put_parts<VEC>(merged, (float)mine, f, sq, ent + (p.slot * nv + p.vec) * (merged ? 1 : VEC));
+    if (p.on) gn_put_parts<VEC>(merged, (float)mine, part, ent + (p.slot * nv + p.vec) * (merged ? 1 : VEC));
     __syncthreads();
     const int per_slot = merged ? nv : nv * VEC;             // parts of a slot
     const int per = merged ? (a.pieces > 1 ? p.width : a.c) / VEC : a.c;   // of them, a group's
     const float each = merged ? (float)VEC : 1.0f;
     const int groups_all = a.G * a.pieces;
-    float2* out = a.part + (p.b * a.chunks + chunk) * groups_all +
+    GnPart* out = a.part + (p.b * a.chunks + chunk) * groups_all +
                   (a.pieces > 1 ? p.slab : p.first);
     gn_join<kGnThreads>(
         p.groups, min(p.slots, nrows), per,
         [&](int s) { return (float)(s < tail ? full + 1 : full) * each; },
         [&](int g, int s, int e) { return ent[s * per_slot + g * per + e]; },
-        [&](int g, float, float mean, float m2) { out[g] = make_float2(mean, m2); });
+        [&](int g, const GnPart& m) { out[g] = m; });
 }
 
-// y = act((x - ref) A + S): A = gamma / sqrt(var + eps), S = beta - (mean -
-// ref) A, from st = (mean - ref, 1 / sqrt(var + eps)).
+// y = act((x - hi) A + S): A = gamma / sqrt(var + eps), S = beta - lo A, from the
+// mean hi + lo and st = (lo, 1 / sqrt(var + eps)).
 __device__ __forceinline__ void gn_factor(float2 st, float gamma, float beta, float& A, float& S) {
     A = st.y * gamma;
     S = fmaf(-st.x, A, beta);
 }
 
-// The cloud's parts in memory, joined: (mean, 1 / deviation) of the slab's
+// The cloud's parts in memory, joined: (lo, 1 / deviation) and hi of the slab's
 // groups.  The first kGnBatch parts of a lane are all on their way at once.
 constexpr int kGnBatch = 8;
 
 template <typename P>
-__device__ __forceinline__ void gn_join_chunks(const GnArgs& a, const P& p, float2* stat) {
+__device__ __forceinline__ void gn_join_chunks(const GnArgs& a, const P& p, float2* stat, float* hi) {
     const int groups_all = a.G * a.pieces;
     const int used = a.by_rows.div((int)p.len - 1) + 1, total = used * a.pieces;
     const int w = gn_lanes<kGnThreads>(p.groups, total);
     const int lane = threadIdx.x & (w - 1), lw = __builtin_ctz(w);
     for (int g = threadIdx.x >> lw; g < p.groups; g += kGnThreads >> lw) {
-        const float2* in = a.part + p.b * a.chunks * groups_all + (p.first + g) * a.pieces;
+        const GnPart* in = a.part + p.b * a.chunks * groups_all + (p.first + g) * a.pieces;
         auto get = [&](int i) {
             const int chunk = a.pieces > 1 ? a.by_pieces.div(i) : i;
             return in[(int64_t)chunk * groups_all + (i - chunk * a.pieces)];
@@ -335,45 +370,51 @@ __device__ __forceinline__ void gn_join_chunks(const GnArgs& a, const P& p, floa
             const int width = a.pieces > 1 ? min(a.slab, a.c - piece * a.slab) : a.c;
             return (float)min(a.chunk_rows, p.len - chunk * a.chunk_rows) * (float)width;
         };
-        float2 keep[kGnBatch];
+        GnPart keep[kGnBatch];
 #pragma unroll
         for (int k = 0; k < kGnBatch; ++k) keep[k] = get(min(lane + k * w, total - 1));
-        const float m0 = get(0).x;
+        GnPart m = get(0);
         float cnt = 0.0f, sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < kGnBatch; ++k)
             if (lane + k * w < total) {
                 const float n = count(lane + k * w);
                 cnt += n;
-                sum += n * (keep[k].x - m0);
+                sum += n * gn_diff(keep[k], m);
             }
         for (int i = lane + kGnBatch * w; i < total; i += w) {
             const float n = count(i);
             cnt += n;
-            sum += n * (get(i).x - m0);
+            sum += n * gn_diff(get(i), m);
         }
         cnt = lane_sum(cnt, w);
-        const float d = lane_sum(sum, w) / cnt;
+        gn_move(m, lane_sum(sum, w) / cnt);
         float m2 = 0.0f;
+        sum = 0.0f;
+        auto add = [&](const GnPart& v, float n) {
+            const float t = gn_diff(v, m), nt = n * t;
+            sum += nt;
+            m2 += v.m2 + nt * t;
+        };
 #pragma unroll
         for (int k = 0; k < kGnBatch; ++k)
-            if (lane + k * w < total) {
-                const float t = (keep[k].x - m0) - d;
-                m2 += keep[k].y + count(lane + k * w) * t * t;
-            }
-        for (int i = lane + kGnBatch * w; i < total; i += w) {
-            const float2 v = get(i);
-            const float t = (v.x - m0) - d;
-            m2 += v.y + count(i) * t * t;
-        }
+            if (lane + k * w < total) add(keep[k], count(lane + k * w));
+        for (int i = lane + kGnBatch * w; i < total; i += w) add(get(i), count(i));
+        sum = lane_sum(sum, w);
         m2 = lane_sum(m2, w);
-        if (lane == 0) stat[g] = make_float2(m0 + d, 1.0f / sqrtf(m2 / cnt + a.eps));
+        const float d = sum / cnt, var = gn_positive(m2 - sum * d) / cnt;
+        gn_move(m, d);
+        if (lane == 0) {
+            stat[g] = make_float2(m.lo, 1.0f / sqrtf(var + a.eps));
+            hi[g] = m.hi;
+        }
     }
 }
 
 template <typename TX, typename TY, int VEC, int ACT>
 __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     __shared__ float2 stat[kGnThreads * VEC];    // a slab's groups: at most its channels
+    __shared__ float hi[kGnThreads * VEC];
     int chunk;
     const int rest = a.by_chunks.div((int)blockIdx.x, chunk);
     const GnPlace<kGnThreads, VEC> p(a, rest);
@@ -381,13 +422,16 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     GnChannels<VEC> c;
     float A[VEC] = {}, S[VEC] = {};
     if (r0 < p.len) {
-        gn_channels<TX, VEC>(a, p, c);
+        p.channel_groups(a, c.grp);
         gn_affine<VEC>(a, p, c);
-        gn_join_chunks(a, p, stat);
+        gn_join_chunks(a, p, stat, hi);
         __syncthreads();
         if (p.on) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) gn_factor(stat[c.grp[k]], c.gamma[k], c.beta[k], A[k], S[k]);
+            for (int k = 0; k < VEC; ++k) {
+                c.ref[k] = hi[c.grp[k]];
+                gn_factor(stat[c.grp[k]], c.gamma[k], c.beta[k], A[k], S[k]);
+            }
         }
     }
     if (!p.on) return;
@@ -406,34 +450,77 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     for (; r < r1; r += p.slots) gn_store(yp + r * a.ldy, GnVec<TY, VEC>{});
 }
 
-// Sums over the workgroup of each group's values, finished once a group: a
-// thread's per channel, then over the rows of its wave, then over waves and
-// channels.  nvp lanes (a power of two) hold a row: a wave several rows, or a
-// row several waves.
-template <int VEC, typename P, typename Finish>
-__device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int nvp, float (&v)[VEC], float* ent,
-                                              float* res, Finish finish) {
+// Sums over the workgroup of each group's values (one or two of each channel),
+// finished once a group: a thread's per channel, or of its channels in one
+// group where a vector lies in one or at most two; then over the rows of its
+// wave, then over waves and entries.  nvp lanes (a power of two) hold a row: a
+// wave several rows, or a row several waves.
+template <int VEC, int VALUES, typename P, typename Finish>
+__device__ __forceinline__ void gn_group_sums(const GnArgs& a, const P& p, int nvp, const int (&grp)[VEC],
+                                              float (&v)[VALUES][VEC], float* ent, Finish finish) {
+    struct alignas(4 * VALUES) Entry {
+        float e[VALUES];
+    };
+    Entry* at = reinterpret_cast<Entry*>(ent);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    // entries of a vector: its groups, or its channels.  Vectors start at multiples of gcd(c, VEC) in their first group.
+    const int low = a.c & -a.c, gcd = low < VEC ? low : VEC;
+    const int units = VEC == 1 || gcd == VEC ? 1 : VEC - gcd <= a.c ? 2 : VEC;
+    if (VEC > 1 && units <= 2) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) v[k] = wave_sum_from(v[k], nvp);
-    const int slots = nvp <= 64 ? kGnOneThreads / 64 : p.slots;
+        for (int i = 0; i < VALUES; ++i) {
+            float s0 = v[i][0], s1 = 0.0f;
+            if (units == 1) {
+#pragma unroll
+                for (int k = 1; k < VEC; ++k) s0 += v[i][k];
+            } else {
+#pragma unroll
+                for (int k = 1; k < VEC; ++k) {
+                    s0 += grp[k] == grp[0] ? v[i][k] : 0.0f;
+                    s1 += grp[k] == grp[0] ? 0.0f : v[i][k];
+                }
+                v[i][VEC > 1 ? 1 : 0] = wave_sum_from(s1, nvp);
+            }
+            v[i][0] = wave_sum_from(s0, nvp);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[i][k] = wave_sum_from(v[i][k], nvp);
+    }
+    const int slots = nvp <= 64 ? kGnOneThreads / 64 : p.slots, row = (int)a.by_nv.d * units;
     const int slot = nvp <= 64 ? wave : p.slot;
     __syncthreads();
     if (p.vec * VEC < p.width && (nvp > 64 || lane < nvp))
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) ent[slot * p.width + p.vec * VEC + k] = v[k];
+        for (int k = 0; k < VEC; ++k)
+            if (k < units) {
+                Entry t;
+#pragma unroll
+                for (int i = 0; i < VALUES; ++i) t.e[i] = v[i][k];
+                at[slot * row + p.vec * units + k] = t;
+            }
     __syncthreads();
-    const int w = gn_lanes<kGnOneThreads>(p.groups, slots * a.c);
+    const int most = units == 1 ? a.c / VEC : units == 2 ? (a.c + VEC - 2) / VEC + 1 : a.c;      // entries of a group
+    const int w = gn_lanes<kGnOneThreads>(p.groups, slots * most);
     int we = 1;
-    while (we < w && we < a.c) we *= 2;
+    while (we < w && we < most) we *= 2;
     const int lw = __builtin_ctz(w), le = __builtin_ctz(we);
     const int l = threadIdx.x & (w - 1), ws = w >> le, s0 = l >> le, e0 = l & (we - 1);
     for (int g = threadIdx.x >> lw; g < p.groups; g += kGnOneThreads >> lw) {
-        float sum = 0.0f;
+        float sum[VALUES] = {};
+        const int first = g * a.c / VEC, per = units == 2 ? (g * a.c + a.c - 1) / VEC - first + 1 : most;
         for (int s = s0; s < slots; s += ws)
-            for (int e = e0; e < a.c; e += we) sum += ent[s * p.width + g * a.c + e];
-        sum = lane_sum(sum, w);
-        if (l == 0) res[g] = finish(sum);
+            for (int e = e0; e < per; e += we) {
+                const int in = units == 2 ? 2 * (first + e) + (a.by_c.div((first + e) * VEC) != g) : g * most + e;
+                const Entry t = at[s * row + in];
+#pragma unroll
+                for (int i = 0; i < VALUES; ++i) sum[i] += t.e[i];
+            }
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) sum[i] = lane_sum(sum[i], w);
+        if (l == 0) finish(g, sum);
     }
     __syncthreads();
 }
@@ -448,11 +535,13 @@ __device__ __forceinline__ void gn_keep(GnVec<T, N>& v) {
 }
 
 // One launch: the slab's valid rows stay in registers between the
-// statistics and the output, so the variance is taken about the mean.
+// statistics and the output.  The first sums estimate the mean, the second ones
+// are of differences to that estimate: their mean corrects it, their squares
+// give the variance.
 template <typename TX, typename TY, int VEC, int ACT, int KEEP>
 __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
-    __shared__ float ent[kGnOneThreads * VEC];   // [slots][width], at most a value for each thread and channel
-    __shared__ float sums[kGnOneThreads * VEC];  // a slab's groups: at most its channels
+    __shared__ float ent[2 * kGnOneThreads * VEC];   // [slots][width], at most two values for each thread and channel
+    __shared__ float2 sums[16 * VEC];    // a slab's groups: at most VEC, or the channels of 16 vectors (the plan)
     const int nv = (int)a.by_nv.d;
     const int shift = nv > 1 ? 32 - __builtin_clz(nv - 1) : 0, nvp = 1 << shift;     // lanes of a row
     // a cloud's slabs share lines of its rows: they go to one XCD
@@ -477,32 +566,34 @@ __global__ __launch_bounds__(kGnOneThreads) void gn_one_kernel(GnArgs a) {
     float A[VEC] = {}, S[VEC] = {};
     if (nrows > 0) {
         const float inv = 1.0f / ((float)nrows * (float)a.c);
-        float v[VEC] = {}, mean[VEC];
+        float v[1][VEC] = {};
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
             if (i < mine)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) v[k] += gn_float(w[i].e[k]) - c.ref[k];
-        gn_group_sums<VEC>(a, p, nvp, v, ent, sums, [&](float sum) { return sum * inv; });
+                for (int k = 0; k < VEC; ++k) v[0][k] += gn_float(w[i].e[k]) - c.ref[k];
+        gn_group_sums<VEC, 1>(a, p, nvp, c.grp, v, ent, [&](int g, const float (&s)[1]) { sums[g].x = s[0] * inv; });
+        float d[2][VEC] = {};
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            mean[k] = sums[c.grp[k]];
-            v[k] = 0.0f;
-        }
+        for (int k = 0; k < VEC; ++k) c.ref[k] += sums[c.grp[k]].x;
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
             if (i < mine) {
                 gn_keep(w[i]);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
-                    const float d = (gn_float(w[i].e[k]) - c.ref[k]) - mean[k];
-                    v[k] = fmaf(d, d, v[k]);
+                    const float t = gn_float(w[i].e[k]) - c.ref[k];
+                    d[0][k] += t;
+                    d[1][k] = fmaf(t, t, d[1][k]);
                 }
             }
         if (KEEP == kGnKeep) gn_affine<VEC>(a, p, c);
-        gn_group_sums<VEC>(a, p, nvp, v, ent, sums, [&](float sum) { return 1.0f / sqrtf(sum * inv + a.eps); });
+        gn_group_sums<VEC, 2>(a, p, nvp, c.grp, d, ent, [&](int g, const float (&s)[2]) {
+            const float lo = s[0] * inv, var = gn_positive(s[1] * inv - lo * lo);
+            sums[g] = make_float2(lo, 1.0f / sqrtf(var + a.eps));
+        });
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) gn_factor(make_float2(mean[k], sums[c.grp[k]]), c.gamma[k], c.beta[k], A[k], S[k]);
+        for (int k = 0; k < VEC; ++k) gn_factor(sums[c.grp[k]], c.gamma[k], c.beta[k], A[k], S[k]);
     }
     if (!p.on) return;
 #pragma unroll
@@ -583,7 +674,7 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
 }
 
 size_t group_norm_ws(const GnPlan& p, int64_t B, int G) {
-    return p.keep ? 0 : ((size_t)(B * p.chunks * G * p.pieces) * 8 + 15) / 16 * 16;
+    return p.keep ? 0 : ((size_t)(B * p.chunks * G * p.pieces) * sizeof(GnPart) + 15) / 16 * 16;
 }
 
 // Widest vector: 16 bytes of x where C allows them, else single values.
@@ -666,7 +757,7 @@ extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype,
     MESO_REQUIRE(launch_fits(ceil_div(B * p.slabs * p.chunks, 8) * 8, p.keep ? kGnOneThreads : kGnThreads), MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
                  (long long)B, (long long)N);
     const int blocks = (int)(B * p.slabs * p.chunks);
-    const GnArgs a = {x, y, lens, gamma, beta, static_cast<float2*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,
+    const GnArgs a = {x, y, lens, gamma, beta, static_cast<GnPart*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,
                       p.slab, p.slabs, p.pieces, p.chunks, p.chunk_rows, blocks, (int)ceil_div(blocks, 8), FastDiv(p.chunks), FastDiv(p.slabs),
                       FastDiv(p.pieces), FastDiv(C / G), FastDiv((unsigned)p.chunk_rows), FastDiv((unsigned)ceil_div(p.slab, vec))};
     hipStream_t s = as_stream(stream);

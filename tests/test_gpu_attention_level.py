@@ -828,3 +828,34 @@ def test_attention_rows_without_a_weight(gpu, dtype, Nq, Nk):
     got = ops.cross_attention(q, k, v)
     within(got[:1], ref, bound)
     assert bool((got[1] == 0).all())
+
+
+# ---------------------------------------------------------------------------
+# group norm: values far from the others
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("N,C,G", [(50, 32, 4), (1023, 192, 32), (5000, 32, 4), (16384, 64, 8), (3000, 30, 3),
+                                   (400, 2064, 1), (70, 6000, 2)])
+@pytest.mark.parametrize("size", [1e3, 1e4, 1e6])
+def test_group_norm_outliers_and_offsets(gpu, dtype, N, C, G, size):
+    """A value far from its group's others, first in the group, in the middle
+    and last, a few leading rows, and an offset of all: every output is as close
+    as the group's values are to their mean.  Sums of at most 200 roundings
+    leave the mean off by 200 u of the values' mean distance to it, and an
+    output by that, by its own distance's roundings and the deviation's."""
+    g = gen(N + C)
+    c = C // G
+    x = randn(g, 6, N, C)
+    x[0, 0, ::c] = size
+    x[1, N // 2, ::c] = -size
+    x[2, N - 1, c - 1::c] = size
+    x[3, :5] *= size
+    x[4] += size
+    x[5, 0, ::c] = -size
+    x[5] += 300.0
+    x = x.to(dtype)
+    y, hat = group_norm_ref(x, G, None, None, 1e-5, "none", None)
+    mean = hat.abs().view(6, N, G, c).mean((1, 3), keepdim=True).expand(6, N, G, c).reshape(6, N, C)
+    bound = 200 * U * (hat.abs() + mean) + (y.abs() * 2.0 ** -8 if dtype == H else 0)
+    within(ops.group_norm(x, G), y, bound)
