@@ -1260,8 +1260,13 @@ AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int 
     // heads) but above 64 channels leave one wave a SIMD (128: 1080 -> 1260 us).  Below a workgroup for most compute
     // units, waves that share 32 rows and split the sources finish sooner (1 x 1024 over 1024, 8 heads of 64: 11 us
     // instead of 22); in fp32, whose shared form is the slower instruction, only for few rows (4 x 349 over 10357, 4
-    // heads on 2, of 24: 79 us with rows of their own, 235 shared).
-    if (dtype == MESORASI_BF16 && D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
+    // heads on 2, of 24: 79 us with rows of their own, 235 shared).  Up to 32 rows, one shared tile, share it however many
+    // clouds and heads there are: three waves of four would have no rows (32 x 1 over 4096, 8 heads of 128: fp32 417 us
+    // with rows of their own, 179 shared, bf16 104 and 102; 32 x 32 over 2048, 8 heads of 64: 98 and 59, 36 and 26; the
+    // other way about 64 x 1 over 1024 of 128 in bf16, 46 and 50; and past 32 rows fp32 64 x 64 over 257 of 32, 22 and 32).
+    if (rows <= 32)
+        p.qb = 0;
+    else if (dtype == MESORASI_BF16 && D <= 64 && pairs * ceil_div(rows, 256) >= 2 * kAtCus)
         p.qb = 2;
     else if (wg1 >= kAtCus * 3 / 4 || (dtype == MESORASI_F32 && rows > 64))
         p.qb = 1;

@@ -720,7 +720,8 @@ def test_offsets_past_32_bits(gpu):
 # ---------------------------------------------------------------------------
 
 @pytest.mark.parametrize("B,Nq,Nk,Hq,Hkv,D", [(2, 1, 50, 8, 2, 64), (1, 7, 2048, 4, 2, 128), (1, 300, 77, 2, 1, 32),
-                                              (1, 40, 1000, 2, 2, 90)])
+                                              (1, 40, 1000, 2, 2, 90), (32, 1, 60, 8, 8, 64), (200, 7, 40, 4, 2, 128),
+                                              (64, 32, 130, 4, 4, 24)])
 def test_attention_few_rows_keep_their_weights(gpu, B, Nq, Nk, Hq, Hkv, D):
     """bf16 rows that share a workgroup: the first of a weight's two bf16 parts is
     rounded down and leaves 2^-7 of it at most, the second half a step of that,
@@ -859,3 +860,17 @@ def test_group_norm_outliers_and_offsets(gpu, dtype, N, C, G, size):
     mean = hat.abs().view(6, N, G, c).mean((1, 3), keepdim=True).expand(6, N, G, c).reshape(6, N, C)
     bound = 200 * U * (hat.abs() + mean) + (y.abs() * 2.0 ** -8 if dtype == H else 0)
     within(ops.group_norm(x, G), y, bound)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("B,Nq,Nk,Hq,Hkv,D", [(32, 1, 300, 8, 8, 128), (100, 1, 70, 4, 2, 64), (64, 16, 97, 4, 4, 40),
+                                              (64, 8, 65, 16, 4, 96), (50, 33, 130, 4, 4, 64), (300, 1, 33, 1, 1, 7)])
+def test_attention_few_rows_of_many_clouds(gpu, dtype, B, Nq, Nk, Hq, Hkv, D):
+    """One query to a few of as many clouds and heads as fill the chip."""
+    g = gen(B + Nq)
+    q, k, v = (randn(g, B, n, h, D, dtype=dtype) for n, h in ((Nq, Hq), (Nk, Hkv), (Nk, Hkv)))
+    k_len = torch.tensor([(b * 11) % (Nk + 1) for b in range(B)], dtype=torch.int32, device="cuda")
+    mask = torch.rand((B, Nk), generator=g, device="cuda") < 0.7
+    within(ops.cross_attention(q, k, v), *_ref_and_bound(q, k, v))
+    kw = dict(k_len=k_len, k_mask=mask)
+    within(ops.cross_attention(q, k, v, **kw), *_ref_and_bound(q, k, v, **kw))
