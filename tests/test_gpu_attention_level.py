@@ -874,3 +874,37 @@ def test_attention_few_rows_of_many_clouds(gpu, dtype, B, Nq, Nk, Hq, Hkv, D):
     within(ops.cross_attention(q, k, v), *_ref_and_bound(q, k, v))
     kw = dict(k_len=k_len, k_mask=mask)
     within(ops.cross_attention(q, k, v, **kw), *_ref_and_bound(q, k, v, **kw))
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit product's large tiles
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+@pytest.mark.parametrize("rows,ci,co", [
+    (4001, 1100, 3003),      # tiles of 256 x 256: 16 x 12 of them, 9 of 128 columns, remainders in all three
+    (12289, 1040, 1025),     # 49 x 5, the last of one row and one channel
+    (3000, 515, 1100),       # tiles of 128 x 128: 24 x 9, 5 of 128 columns
+    (25000, 131, 67),        # 196 x 1, two of 128 columns, the second of 16
+    (2500, 2000, 1409),      # 20 x 12, 16 of 128 columns
+])
+def test_linear_large_tiles(gpu, dtype, rows, ci, co):
+    """Sizes for each of the large tiles, with several steps over the columns
+    and with remainders; the bound of test_linear."""
+    g = gen(rows + ci)
+    W = randn(g, co, ci) / math.sqrt(ci)
+    b = randn(g, co)
+    p = ops.Int8Params.from_float(W, b)
+    x = randn(g, rows, ci, dtype=H if dtype == "bf16" else F) * torch.exp(randn(g, rows, 1)).to(H if dtype == "bf16" else F)
+    q, s = quantize_ref(x)
+    wq, ws = quantize_ref(W)
+    prod = (q.double() @ wq.double().t()) * s.double()[:, None] * ws.double()[None]
+    xin, xs = (ops.int8_rows(q), s) if dtype == "i8" else (x, None)
+    for relu, out in ((False, F), (True, H)):
+        ref = prod + b.double()
+        ref = torch.clamp_min(ref, 0) if relu else ref
+        bound = 4 * U * (prod.abs() + ref.abs()) + (ref.abs() * 2.0 ** -8 if out == H else 0) + 1e-30
+        buf = torch.full((rows + 1, co + 1), 5.0, dtype=out, device="cuda")
+        ops.linear_int8(xin, p, x_scale=xs, relu=relu, out_dtype=out, out=buf[:rows, :co])
+        within(buf[:rows, :co], ref, bound)
+        assert bool((buf[rows] == 5).all() and (buf[:, co] == 5).all())
