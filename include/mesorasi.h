@@ -539,12 +539,14 @@ int mesorasi_count_out_of_range(const int32_t* idx, int64_t n, int32_t bound, in
  *   gamma, beta [C] float32, nullable (1 and 0)
  *   act   MESORASI_ACT_*: none, max(y, 0), y / (1 + exp(-y)), or
  *         y (1 + erf(y / sqrt 2)) / 2
- *   y     [B, N, ld_y] of y_dtype (F32 or BF16)
+ *   y     [B, N, ld_y] of y_dtype (F32 or BF16); must not overlap x (other
+ *         columns of its rows are apart)
  *   ws    at least mesorasi_group_norm_workspace() bytes, 16-byte aligned
  *         (NULL allowed when that size is 0; any contents on entry); calls
  *         that overlap in time need separate workspaces
  * Errors: EINVAL for NULL x/y, sizes < 0, C < 1, G < 1, C % G != 0, ld < C,
- *         an unknown act, eps negative or not finite, a misaligned ws;
+ *         an unknown act, eps negative or not finite, a misaligned ws, y that
+ *         overlaps x;
  *         EUNSUPPORTED for an unknown dtype, C > MESORASI_MAX_C_NORM, N or
  *         B > 2^31 - 1, or more work than one launch holds; EWORKSPACE when
  *         ws is too small.
@@ -568,8 +570,9 @@ size_t mesorasi_group_norm_workspace(int64_t B, int64_t N, int32_t C, int32_t G,
  *   q     [rows, ld_q] int8 out, 16-byte aligned, ld_q a multiple of 16;
  *         columns C .. up to the next multiple of 16 are written as 0
  *   scale [rows] float32 out
+ *         Neither may overlap x.
  * Errors: EINVAL for NULL pointers, rows < 0, C < 1, ld_x < C, ld_q < C or
- *         not a multiple of 16, a misaligned q; EUNSUPPORTED for an unknown
+ *         not a multiple of 16, a misaligned q, an overlap; EUNSUPPORTED for an unknown
  *         dtype, C > MESORASI_MAX_WIDTH_I8, rows > 2^31 - 1 or more work than
  *         one launch holds.
  */
@@ -592,14 +595,14 @@ int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype, int64_t r
  *         aligned, ld_w a multiple of 16, columns c_in .. up to the next
  *         multiple of 16 hold 0;  w_scale [c_out] float32
  *   bias  [c_out] float32, nullable
- *   y     [rows, ld_y] of y_dtype (F32 or BF16)
+ *   y     [rows, ld_y] of y_dtype (F32 or BF16); must not overlap an input
  *   ws    at least mesorasi_linear_i8_workspace() bytes, 16-byte aligned
  *         (NULL allowed when that size is 0; any contents on entry); calls
  *         that overlap in time need separate workspaces
  * Errors: EINVAL for NULL x/W/w_scale/y, rows < 0, c_in < 1, c_out < 1,
  *         ld < width, an ld_w (or an I8 ld_x) that is no multiple of 16, a
  *         misaligned W, ws or I8 x, x_scale missing (I8) or given
- *         (F32, BF16); EUNSUPPORTED for an unknown dtype, a width above
+ *         (F32, BF16), y that overlaps x, x_scale or W; EUNSUPPORTED for an unknown dtype, a width above
  *         MESORASI_MAX_WIDTH_I8, rows > 2^31 - 1 or more work than one launch
  *         holds; EWORKSPACE when ws is too small.
  */
@@ -626,10 +629,12 @@ size_t mesorasi_linear_i8_workspace(int64_t rows, int32_t c_in, int32_t c_out, i
  *   pos   [rows, ld_pos] float32 (first n_axes columns)
  *   sections host array [n_axes], each >= 0
  *   freq  [P] float32
- *   y     [rows, ld_y] of dtype; may be x itself when ld_y == ld_x
+ *   y     [rows, ld_y] of dtype; may be x itself when ld_y == ld_x, must not
+ *         overlap an input otherwise
  * Errors: EINVAL for NULL pointers, rows < 0, H < 1, D < 1, ld < width, a
  *         negative section, P < 1, 2 P > D, y == x with another leading
- *         dimension; EUNSUPPORTED for an unknown dtype, n_axes outside
+ *         dimension, y that overlaps x in another way, or pos or freq;
+ *         EUNSUPPORTED for an unknown dtype, n_axes outside
  *         [1, MESORASI_MAX_AXES], D > MESORASI_MAX_D_ROTARY, H > 65536, rows >
  *         2^31 - 1 or more work than one launch holds.
  */
@@ -658,6 +663,7 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  *         heads may lie side by side in a row or one after another, k and v may
  *         be columns of one projection, and a set may be the filled part of a
  *         longer buffer.  Input strides may be 0 (shared by clouds or heads).
+ *         o must not overlap q, k or v (other columns of their rows are apart).
  *   k_len  [B] int32 or NULL (all Nk); a value outside [0, Nk] is taken as the
  *         nearest of the two
  *   k_mask [B, mask_ld] bytes or NULL (all valid)
@@ -667,7 +673,8 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  * Errors: EINVAL for NULL q/k/v/o, sizes < 0, Hq < 1, Hkv < 1,
  *         Hq % Hkv != 0, D < 1, a negative stride, an output stride < D (over
  *         more than one cloud, point or head), mask_ld < Nk with a mask and
- *         more than one cloud, a scale that is not finite, a misaligned ws;  EUNSUPPORTED for an unknown dtype,
+ *         more than one cloud, a scale that is not finite, a misaligned ws, o
+ *         that overlaps q, k or v;  EUNSUPPORTED for an unknown dtype,
  *         D > MESORASI_MAX_D_ATTN, Nq (Hq / Hkv) or Nk > 2^31 - 1024, or more
  *         work than one launch holds;  EWORKSPACE when ws is too small.
  *         Nk == 0 is valid: every output is 0.

@@ -1417,6 +1417,14 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     MESO_REQUIRE(launch_fits(8 * per, kAtThreads), MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: %lld workgroups",
                  (long long)p.blocks);
     a.per_xcd = (int)per;
+    const int elem = dtype == MESORASI_F32 ? 4 : 2;
+    auto extent = [&](const void* t, int64_t n, int64_t heads, int64_t bs, int64_t ld, int64_t hs) {
+        return Extent{t, (int64_t)D * elem, {B, n, heads}, {bs * elem, ld * elem, hs * elem}};
+    };
+    const Extent ext = extent(o, Nq, Hq, o_bs, o_ld, o_hs);
+    MESO_REQUIRE(!overlap(ext, extent(q, Nq, Hq, q_bs, q_ld, q_hs)) && !overlap(ext, extent(k, Nk, Hkv, k_bs, k_ld, k_hs)) &&
+                     !overlap(ext, extent(v, Nk, Hkv, v_bs, v_ld, v_hs)),
+                 MESORASI_EINVAL, "mesorasi_cross_attention: o overlaps q, k or v");
     // 16-byte pieces of every row, runs of 4 channels of the output
     const bool f32 = dtype == MESORASI_F32;
     const int64_t st = q_bs | q_ld | q_hs | k_bs | k_ld | k_hs | v_bs | v_ld | v_hs | D;

@@ -27,6 +27,56 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // A launch holds fewer than 2^32 threads.
 inline bool launch_fits(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
 
+// Where a tensor's elements lie: n[i] runs of `width` bytes, stride[i] bytes
+// apart, in up to three dimensions.
+struct Extent {
+    const void* p;
+    int64_t width;
+    int64_t n[3], stride[3];
+};
+
+inline Extent rows_extent(const void* p, int64_t rows, int64_t ld, int64_t width, int elem) {
+    return {p, width * elem, {rows, 1, 1}, {ld * elem, 0, 0}};
+}
+
+// Two tensors may share bytes: they do not where their address ranges are
+// apart, or where both repeat with one pitch (a stride of either) and lie in
+// different columns of it.
+inline bool overlap(const Extent& a, const Extent& b) {
+    const Extent* t[2] = {&a, &b};
+    uint64_t lo[2], hi[2];
+    for (int i = 0; i < 2; ++i) {
+        int64_t span = t[i]->width;
+        for (int d = 0; d < 3; ++d) {
+            if (t[i]->n[d] < 1) return false;
+            span += (t[i]->n[d] - 1) * t[i]->stride[d];
+        }
+        lo[i] = reinterpret_cast<uintptr_t>(t[i]->p);
+        hi[i] = lo[i] + (uint64_t)span;
+    }
+    if (!t[0]->p || !t[1]->p || hi[0] <= lo[1] || hi[1] <= lo[0]) return false;
+    for (int c = 0; c < 6; ++c) {
+        const int64_t pitch = t[c / 3]->n[c % 3] > 1 ? t[c / 3]->stride[c % 3] : 0;
+        int64_t in[2];
+        bool whole = pitch > 0;
+        for (int i = 0; i < 2 && whole; ++i) {
+            in[i] = t[i]->width;                     // bytes within the pitch
+            for (int d = 0; d < 3; ++d) {
+                if (t[i]->n[d] <= 1) continue;
+                if (t[i]->stride[d] < pitch)
+                    in[i] += (t[i]->n[d] - 1) * t[i]->stride[d];
+                else
+                    whole = whole && t[i]->stride[d] % pitch == 0;
+            }
+            whole = whole && in[i] <= pitch;
+        }
+        if (!whole) continue;
+        const int64_t at = (int64_t)((lo[1] % (uint64_t)pitch + (uint64_t)pitch - lo[0] % (uint64_t)pitch) % (uint64_t)pitch);
+        if (at >= in[0] && at + in[1] <= pitch) return false;
+    }
+    return true;
+}
+
 inline bool aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; }
 
 // Zero-fill of a strided [rows, cols] float32 region (used before pooled

@@ -756,6 +756,8 @@ extern "C" int mesorasi_group_norm(const void* x, int64_t ld_x, int32_t x_dtype,
     MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_group_norm: ws is not 16-byte aligned");
     MESO_REQUIRE(launch_fits(ceil_div(B * p.slabs * p.chunks, 8) * 8, p.keep ? kGnOneThreads : kGnThreads), MESORASI_EUNSUPPORTED, "mesorasi_group_norm: B = %lld, N = %lld",
                  (long long)B, (long long)N);
+    MESO_REQUIRE(!overlap(rows_extent(x, B * N, ld_x, C, ex), rows_extent(y, B * N, ld_y, C, ey)), MESORASI_EINVAL,
+                 "mesorasi_group_norm: y overlaps x");
     const int blocks = (int)(B * p.slabs * p.chunks);
     const GnArgs a = {x, y, lens, gamma, beta, static_cast<GnPart*>(ws), ld_x, ld_y, B, N, C, G, C / G, eps, act,
                       p.slab, p.slabs, p.pieces, p.chunks, p.chunk_rows, blocks, (int)ceil_div(blocks, 8), FastDiv(p.chunks), FastDiv(p.slabs),

@@ -543,6 +543,9 @@ extern "C" int mesorasi_quantize_i8(const void* x, int64_t ld_x, int32_t x_dtype
     if (rows == 0) return MESORASI_OK;
     MESO_REQUIRE(x && q && scale, MESORASI_EINVAL, "mesorasi_quantize_i8: NULL pointer");
     MESO_REQUIRE(aligned(q, 16), MESORASI_EINVAL, "mesorasi_quantize_i8: q is not 16-byte aligned");
+    const Extent ext = rows_extent(x, rows, ld_x, C, x_dtype == MESORASI_F32 ? 4 : 2);
+    MESO_REQUIRE(!overlap(ext, rows_extent(q, rows, ld_q, i8_pad(C), 1)) && !overlap(ext, rows_extent(scale, rows, 1, 1, 4)),
+                 MESORASI_EINVAL, "mesorasi_quantize_i8: q or scale overlaps x");
     run_quantize(x, ld_x, x_dtype, rows, C, q, ld_q, scale, as_stream(stream));
     return after_launch("mesorasi_quantize_i8");
 }
@@ -582,6 +585,15 @@ extern "C" int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, 
     hipStream_t s = as_stream(stream);
     const int kp = (int)i8_pad(c_in);
     const bool f32 = y_dtype == MESORASI_F32;
+    const size_t need = mesorasi_linear_i8_workspace(rows, c_in, c_out, x_dtype);
+    MESO_REQUIRE(need == 0 || (ws && ws_bytes >= need), MESORASI_EWORKSPACE,
+                 "mesorasi_linear_i8: workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+    MESO_REQUIRE(need == 0 || aligned(ws, 16), MESORASI_EINVAL, "mesorasi_linear_i8: ws is not 16-byte aligned");
+    const int elem = x_dtype == MESORASI_F32 ? 4 : x_dtype == MESORASI_BF16 ? 2 : 1;
+    const Extent ext = rows_extent(y, rows, ld_y, c_out, f32 ? 4 : 2);
+    MESO_REQUIRE(!overlap(ext, rows_extent(x, rows, ld_x, c_in, elem)) && !overlap(ext, rows_extent(W, c_out, ld_w, c_in, 1)) &&
+                     !overlap(ext, rows_extent(x_scale, rows, 1, 1, 4)),
+                 MESORASI_EINVAL, "mesorasi_linear_i8: y overlaps an input");
     LinArgs a = {static_cast<const int8_t*>(x), x_scale, W, w_scale, bias, y, ld_x, ld_w, ld_y, rows, kp, c_out, relu};
     if (linear_few_fused(rows, kp, x_dtype)) {
         if (x_dtype == MESORASI_F32) {
@@ -595,10 +607,6 @@ extern "C" int mesorasi_linear_i8(const void* x, int64_t ld_x, int32_t x_dtype, 
         return after_launch("mesorasi_linear_i8");
     }
     if (x_dtype != MESORASI_I8) {
-        const size_t need = mesorasi_linear_i8_workspace(rows, c_in, c_out, x_dtype);
-        MESO_REQUIRE(ws && ws_bytes >= need, MESORASI_EWORKSPACE, "mesorasi_linear_i8: workspace %zu < %zu bytes",
-                     ws ? ws_bytes : (size_t)0, need);
-        MESO_REQUIRE(aligned(ws, 16), MESORASI_EINVAL, "mesorasi_linear_i8: ws is not 16-byte aligned");
         int8_t* q = static_cast<int8_t*>(ws);
         float* qs = reinterpret_cast<float*>(q + rows * kp);
         run_quantize(x, ld_x, x_dtype, rows, c_in, q, kp, qs, s);

@@ -188,12 +188,12 @@ extern "C" int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64
                  "mesorasi_rotary: y == x with another leading dimension");
     if (rows == 0) return MESORASI_OK;
     MESO_REQUIRE(x && y && pos && freq, MESORASI_EINVAL, "mesorasi_rotary: NULL pointer");
+    const int elem = dtype == MESORASI_F32 ? 4 : 2;
     a.x = x; a.y = y; a.pos = pos; a.freq = freq;
     a.ldx = ld_x; a.ldy = ld_y; a.ldp = ld_pos; a.rows = rows;
     a.H = H; a.D = D; a.P = (int)P; a.n_axes = n_axes;
     a.copy = x != y && 2 * P < D;
     // the widest vector that divides every run of channels and is aligned
-    const int elem = dtype == MESORASI_F32 ? 4 : 2;
     int vec = 16 / elem;
     while (vec > 1 && !(P % vec == 0 && D % vec == 0 && ld_x % vec == 0 && ld_y % vec == 0 &&
                         aligned(x, vec * elem) && aligned(y, vec * elem)))
@@ -211,6 +211,10 @@ extern "C" int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64
     a.tpr = tpr;
     MESO_REQUIRE(launch_fits(ceil_div(rows, R), kRotThreads), MESORASI_EUNSUPPORTED, "mesorasi_rotary: %lld rows of %lld pairs",
                  (long long)rows, (long long)P);
+    const Extent ext = rows_extent(y, rows, ld_y, width, elem);
+    MESO_REQUIRE((x == y || !overlap(ext, rows_extent(x, rows, ld_x, width, elem))) &&
+                     !overlap(ext, rows_extent(pos, rows, ld_pos, n_axes, 4)) && !overlap(ext, rows_extent(freq, 1, P, P, 4)),
+                 MESORASI_EINVAL, "mesorasi_rotary: y overlaps an input");
     const unsigned grid = (unsigned)ceil_div(rows, R);
     hipStream_t s = as_stream(stream);
     if (dtype == MESORASI_F32) {

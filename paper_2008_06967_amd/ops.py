@@ -642,7 +642,8 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
     """Group norm over each cloud's valid points with an activation ("none",
     "relu", "silu", "gelu").  x [B, N, C] float32 or bfloat16; gamma, beta
     [C] float32; lens [B] int32 (rows from lens[b] on are not read and come
-    out 0).  out: like x, or of the other type (see the C header); not x."""
+    out 0).  out: like x, or of the other type (see the C header); it may not
+    overlap x, other columns of its rows aside."""
     _require(x.dim() == 3, "x must be [B, N, C]")
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
@@ -669,7 +670,8 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
 def quantize_int8(x: torch.Tensor, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
     """Rows in 8 bits with a scale each: (q, scale) of x [..., C] float32 or
     bfloat16.  q [..., C] int8 has rows a multiple of 16 bytes apart, as
-    linear_int8 reads them."""
+    linear_int8 reads them; the bytes behind each row up to the next multiple of
+    16 are written as 0, in a given out too.  Neither may overlap x."""
     dt = _dtype(x, "x")
     px, ldx = _ld(x, "x")
     C, lead = x.shape[-1], x.shape[:-1]
@@ -754,7 +756,7 @@ def linear_int8(x: torch.Tensor, p: Int8Params, x_scale: torch.Tensor | None = N
     """A layer's product in 8-bit integers.  x [..., C_in] float32 or
     bfloat16 (brought to 8 bits within the call), or int8 rows of
     quantize_int8() with their x_scale.  out_dtype: float32 (the default) or
-    bfloat16."""
+    bfloat16.  out may not overlap an input."""
     int8 = x.dtype is torch.int8
     dt = I8 if int8 else _dtype(x, "x")
     *lead, c_in = x.shape
@@ -805,7 +807,7 @@ class RotaryParams:
 def rotary(x: torch.Tensor, pos: torch.Tensor, p: RotaryParams, out: torch.Tensor | None = None):
     """Every head's feature pairs turned by the row's coordinates.  x [..., H,
     D] float32 or bfloat16, heads side by side; pos [..., axes] float32.  out
-    may be x."""
+    may be x, but not overlap an input in another way."""
     dt = _dtype(x, "x")
     shape = x.shape
     _require(len(shape) >= 2, "x must be [..., H, D]")
@@ -861,7 +863,8 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     layout transposed, the filled part of a longer buffer).  k_len [B] int32:
     sources from k_len[b] on are not valid; k_mask [B, Nk] bool: only the True
     ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
-    unless given.  out: like q (its strides may differ), not q, k or v."""
+    unless given.  out: like q (its strides may differ); it may not overlap q, k
+    or v, other columns of their rows aside."""
     qs, ks = q.shape, k.shape
     _require(len(qs) == 4 and len(ks) == 4 and v.shape == ks, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
     B, Nq, Hq, D = qs

@@ -471,6 +471,56 @@ def test_cross_attention_validation_and_workspace():
     assert L.mesorasi_cross_attention_workspace(2, -4, 16, 4, 2, 64, 1) == 0
 
 
+def test_outputs_over_inputs():
+    """An output that shares bytes with an input is refused, whatever its
+    start."""
+    at = lambda i: ctypes.c_void_p(0x100000 + i)
+    x = at(0)
+
+    def gn(y, ldx=64, ldy=64, xd=0, yd=0, B=2, N=100):
+        return st("mesorasi_group_norm", x, ldx, xd, B, N, 32, 8, NULL, NULL, NULL, 1e-5, 0, y, ldy, yd, at(1 << 24),
+                  1 << 20, NULL)
+
+    for i in (0, 4, 112, 256, 256 * 199, -256, -256 * 199):
+        assert gn(at(i)) == _lib.EINVAL, i
+    assert gn(at(64), yd=1) == _lib.EINVAL and gn(at(128), ldy=32) == _lib.EINVAL
+
+    def qu(q, s=at(1 << 20)):
+        return st("mesorasi_quantize_i8", x, 100, 0, 10, 100, q, 112, s, NULL)
+
+    for i in (0, 16, 3984, -112, -1008):
+        assert qu(at(i)) == _lib.EINVAL, i
+    assert qu(at(1 << 16), at(396)) == _lib.EINVAL
+
+    def lin(y, W=at(1 << 20), xd=0, xs=NULL):
+        return st("mesorasi_linear_i8", x, 112, xd, xs, 10, 100, W, 112, at(1 << 21), NULL, 50, 0, y, 64, 0, at(1 << 24),
+                  1 << 20, NULL)
+
+    for i in (0, 4, 48 * 4, 9 * 448, -4 * 64):
+        assert lin(at(i)) == _lib.EINVAL, i
+    assert lin(at(1 << 16), W=at((1 << 16) + 2496)) == _lib.EINVAL
+    assert lin(at(1 << 16), xd=2, xs=at((1 << 16) - 36)) == _lib.EINVAL
+
+    S = (ctypes.c_int32 * 1)(8)
+
+    def rot(y, pos=at(1 << 20), freq=at(1 << 21)):
+        return st("mesorasi_rotary", x, 64, 0, 10, 2, 16, pos, 1, 1, S, freq, 0, y, 64, NULL)
+
+    for i in (4, 64, 256, 192, -256 * 9):
+        assert rot(at(i)) == _lib.EINVAL, i
+    assert rot(at(1 << 16), pos=at((1 << 16) + 2400)) == _lib.EINVAL
+    assert rot(at(1 << 16), freq=at((1 << 16) + 124)) == _lib.EINVAL
+
+    def att(o, q=x, k=at(1 << 20), v=at(1 << 21), os=(2816, 256, 64)):
+        return st("mesorasi_cross_attention", q, 2816, 256, 64, k, 2816, 256, 64, v, 2816, 256, 64, 0, 2, 11, 11, 2, 2, 48,
+                  1.0, NULL, NULL, 0, o, *os, at(1 << 24), 1 << 20, NULL)
+
+    for t in (0, 1 << 20, 1 << 21):
+        for i in (0, 4, 256, 1024 * 10, 1024 * 21, -1024 * 21, 188):
+            assert att(at(t + i)) == _lib.EINVAL, (t, i)
+    assert att(at(512), os=(11 * 128, 128, 64)) == _lib.EINVAL
+
+
 def test_more_work_than_one_launch_holds():
     """2^32 threads and up are refused before any HIP call."""
     big = 0x7fffffff

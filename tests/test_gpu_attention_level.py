@@ -908,3 +908,45 @@ def test_linear_large_tiles(gpu, dtype, rows, ci, co):
         ops.linear_int8(xin, p, x_scale=xs, relu=relu, out_dtype=out, out=buf[:rows, :co])
         within(buf[:rows, :co], ref, bound)
         assert bool((buf[rows] == 5).all() and (buf[:, co] == 5).all())
+
+
+# ---------------------------------------------------------------------------
+# outputs beside and over inputs
+# ---------------------------------------------------------------------------
+
+def test_outputs_beside_inputs(gpu):
+    """Other columns or rows of an input's buffer take the output; views that
+    share bytes with an input are refused."""
+    g = gen(40)
+    buf = randn(g, 2, 60, 96)
+    x = buf[..., :32]
+    for out in (buf[..., 32:64], buf[..., 64:96]):
+        ref = ops.group_norm(x.clone(), 8)
+        assert torch.equal(ops.group_norm(x, 8, out=out), ref)
+    flat = buf.view(120, 96)
+    p = ops.Int8Params.from_float(randn(g, 40, 32))
+    ref = ops.linear_int8(flat[::2, :32].clone(), p)
+    assert torch.equal(ops.linear_int8(flat[::2, :32], p, out=flat[::2, 32:72]), ref)
+    assert torch.equal(ops.linear_int8(flat[::2, :32], p, out=flat[1::2, :40]), ref)
+    r = ops.RotaryParams([8])
+    pos = randn(g, 120, 1)
+    h = flat.view(120, 6, 16)
+    ref = ops.rotary(h[:, :2].clone(), pos, r)
+    assert torch.equal(ops.rotary(h[:, :2], pos, r, out=h[:, 2:4]), ref)
+    qkvo = randn(g, 2, 50, 4, 3, 16)
+    q, k, v, o = (qkvo[:, :, i] for i in range(4))
+    ref = ops.cross_attention(q.clone(), k, v)
+    assert torch.equal(ops.cross_attention(q, k, v, out=o), ref)
+    heads = randn(g, 2, 4, 50, 16).transpose(1, 2)          # clouds, points, heads: one after another
+    ref = ops.cross_attention(heads[:, :, :2].clone(), k[:, :, :2], v[:, :, :2])
+    assert torch.equal(ops.cross_attention(heads[:, :, :2], k[:, :, :2], v[:, :, :2], out=heads[:, :, 2:]), ref)
+    before = buf.clone()
+    for f in (lambda: ops.group_norm(x, 8, out=buf[..., 16:48]),
+              lambda: ops.group_norm(buf[:1, :59], 8, out=buf[:1, 1:]),
+              lambda: ops.linear_int8(flat[:60, :32], p, out=flat[30:90, 24:64]),
+              lambda: ops.rotary(h[:119], pos[:119], r, out=h[1:]),
+              lambda: ops.rotary(h[:, :2], pos, r, out=h[:, 1:3]),
+              lambda: ops.cross_attention(q, k, v, out=qkvo.view(2, 50, 12, 16)[:, :, 8:11])):
+        with pytest.raises(_lib.MesorasiError, match="overlaps"):
+            f()
+    assert torch.equal(buf, before)
