@@ -84,8 +84,8 @@ __device__ __forceinline__ int at_swz(int row) {
 // 16 bytes from each lane's address to LDS at base + 16 lane.  The wait is
 // the caller's: at_wait_loads() before the barrier that publishes the tile.
 __device__ __forceinline__ void at_load_lds(const void* g, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(g)
-                 : "memory");
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(uintptr_t)g,
+                                     (__attribute__((address_space(3))) uint32_t*)(uintptr_t)lds_base, 16, 0, 0);
 }
 __device__ __forceinline__ void at_wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 

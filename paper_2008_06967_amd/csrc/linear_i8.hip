@@ -195,8 +195,8 @@ constexpr int kLinK = 128;           // bytes of a row in a tile: eight 16-byte 
 __device__ __forceinline__ int lin_swz(int row) { return (row >> 1) & 7; }
 
 __device__ __forceinline__ void lin_load_lds(const void* g, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(g)
-                 : "memory");
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(uintptr_t)g,
+                                     (__attribute__((address_space(3))) uint32_t*)(uintptr_t)lds_base, 16, 0, 0);
 }
 
 // Four channels of a row: scaled, biased (a missing bias is 0: adding it
