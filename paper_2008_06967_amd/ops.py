@@ -555,8 +555,6 @@ def _like(t, x: torch.Tensor, name: str, dtype, shape):
 
 
 _entry_points: dict = {}
-_this_device = torch._C._cuda_getDevice
-_this_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _entry(name: str):
@@ -570,12 +568,13 @@ def _call(x: torch.Tensor, where: str, *args):
     """The entry point `where` on x's device, on that device's current stream."""
     if not x.is_cuda:
         raise ValueError(f"{where}: tensors must be on a GPU, not on {x.device}")
-    fn, i = _entry(where), x.get_device()
-    if i == _this_device():
-        rc = fn(*args, _this_stream(i))
+    # less host work than torch.cuda's own wrappers, looked up here: a torch built without a GPU has neither
+    fn, i, device, stream = _entry(where), x.get_device(), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    if i == device():
+        rc = fn(*args, stream(i))
     else:
         with torch.cuda.device(i):
-            rc = fn(*args, _this_stream(i))
+            rc = fn(*args, stream(i))
     if rc:
         check(rc, where)
 

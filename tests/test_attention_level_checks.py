@@ -107,3 +107,23 @@ def test_out_must_not_be_an_input():
     # other columns of one buffer are apart: the call goes on to the device check
     with pytest.raises(ValueError, match="must be on a GPU"):
         ops.group_norm(x[..., :8], 4, out=x[..., 8:])
+
+
+def test_import_without_gpu_functions():
+    """The module loads, and refuses CPU tensors, on a torch that lacks the
+    GPU build's functions."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = ("import torch\n"
+            "for n in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    if hasattr(torch._C, n): delattr(torch._C, n)\n"
+            "from paper_2008_06967_amd import ops\n"
+            "try:\n"
+            "    ops.group_norm(torch.zeros(1, 5, 8), 2)\n"
+            "except ValueError as e:\n"
+            "    assert 'GPU' in str(e)\n"
+            "    print('refused')\n")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "refused" in r.stdout, r.stderr[-2000:]
