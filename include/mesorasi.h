@@ -666,14 +666,15 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  *         o must not overlap q, k or v (other columns of their rows are apart).
  *   k_len  [B] int32 or NULL (all Nk); a value outside [0, Nk] is taken as the
  *         nearest of the two
- *   k_mask [B, mask_ld] bytes or NULL (all valid)
+ *   k_mask [B, mask_ld] bytes or NULL (all valid); mask_ld may be 0 (shared by
+ *         clouds)
  *   ws    at least mesorasi_cross_attention_workspace() bytes, 16-byte aligned
  *         (NULL allowed when that size is 0; any contents on entry); calls
  *         that overlap in time need separate workspaces
  * Errors: EINVAL for NULL q/k/v/o, sizes < 0, Hq < 1, Hkv < 1,
  *         Hq % Hkv != 0, D < 1, a negative stride, an output stride < D (over
- *         more than one cloud, point or head), mask_ld < Nk with a mask and
- *         more than one cloud, a scale that is not finite, a misaligned ws, o
+ *         more than one cloud, point or head), mask_ld < Nk and not 0 with a
+ *         mask and more than one cloud, a scale that is not finite, a misaligned ws, o
  *         that overlaps q, k or v;  EUNSUPPORTED for an unknown dtype,
  *         D > MESORASI_MAX_D_ATTN, Nq (Hq / Hkv) or Nk > 2^31 - 1024, or more
  *         work than one launch holds;  EWORKSPACE when ws is too small.

@@ -1388,7 +1388,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
                  MESORASI_EINVAL, "mesorasi_cross_attention: negative stride");
     MESO_REQUIRE((B <= 1 || o_bs >= D) && (Nq <= 1 || o_ld >= D) && (Hq <= 1 || o_hs >= D), MESORASI_EINVAL,
                  "mesorasi_cross_attention: an output stride < D");
-    MESO_REQUIRE(!k_mask || B <= 1 || mask_ld >= Nk, MESORASI_EINVAL, "mesorasi_cross_attention: mask_ld < Nk");
+    MESO_REQUIRE(!k_mask || B <= 1 || mask_ld == 0 || mask_ld >= Nk, MESORASI_EINVAL, "mesorasi_cross_attention: mask_ld < Nk");
     MESO_REQUIRE(std::isfinite(scale), MESORASI_EINVAL, "mesorasi_cross_attention: scale = %g", (double)scale);
     MESO_REQUIRE(dtype == MESORASI_F32 || dtype == MESORASI_BF16, MESORASI_EUNSUPPORTED,
                  "mesorasi_cross_attention: dtype %d", dtype);

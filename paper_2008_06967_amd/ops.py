@@ -641,7 +641,8 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, 
     """Group norm over each cloud's valid points with an activation ("none",
     "relu", "silu", "gelu").  x [B, N, C] float32 or bfloat16; gamma, beta
     [C] float32; lens [B] int32 (rows from lens[b] on are not read and come
-    out 0).  out: like x, or of the other type (see the C header); it may not
+    out 0).  The rows of x and of out are evenly spaced, across
+    clouds too.  out: like x, or of the other type (see the C header); it may not
     overlap x, other columns of its rows aside."""
     _require(x.dim() == 3, "x must be [B, N, C]")
     if act not in _ACTS:
@@ -805,7 +806,8 @@ class RotaryParams:
 
 def rotary(x: torch.Tensor, pos: torch.Tensor, p: RotaryParams, out: torch.Tensor | None = None):
     """Every head's feature pairs turned by the row's coordinates.  x [..., H,
-    D] float32 or bfloat16, heads side by side; pos [..., axes] float32.  out
+    D] float32 or bfloat16, heads side by side; pos [..., axes] float32; the
+    leading dimensions of each collapse into evenly spaced rows.  out
     may be x, but not overlap an input in another way."""
     dt = _dtype(x, "x")
     shape = x.shape
@@ -860,8 +862,8 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     k, v [B, Nk, Hkv, D], Hq a multiple of Hkv; float32 or bfloat16, any
     strides with contiguous channels (views of one projection, a head-major
     layout transposed, the filled part of a longer buffer).  k_len [B] int32:
-    sources from k_len[b] on are not valid; k_mask [B, Nk] bool: only the True
-    ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
+    sources from k_len[b] on are not valid; k_mask [B, Nk] bool (its
+    clouds may share one row): only the True ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
     unless given.  out: like q (its strides may differ); it may not overlap q, k
     or v, other columns of their rows aside."""
     qs, ks = q.shape, k.shape

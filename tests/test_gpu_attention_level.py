@@ -950,3 +950,15 @@ def test_outputs_beside_inputs(gpu):
         with pytest.raises(_lib.MesorasiError, match="overlaps"):
             f()
     assert torch.equal(buf, before)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("Nq,Nk", [(1, 700), (150, 130)])
+def test_attention_shared_mask(gpu, dtype, Nq, Nk):
+    """One row of a mask for all clouds, without a copy."""
+    g = gen(41)
+    q, k, v = (randn(g, 3, n, h, 32, dtype=dtype) for n, h in ((Nq, 4), (Nk, 2), (Nk, 2)))
+    mask = (torch.rand((1, Nk), generator=g, device="cuda") < 0.5).expand(3, Nk)
+    got = ops.cross_attention(q, k, v, k_mask=mask)
+    within(got, *_ref_and_bound(q, k, v, k_mask=mask))
+    assert torch.equal(got, ops.cross_attention(q, k, v, k_mask=mask.contiguous()))
