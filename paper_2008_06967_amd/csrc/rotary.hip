@@ -2,9 +2,10 @@
 //
 // Pair j of a head turns by t = pos[r, axis(j)] freq[j], the same for every
 // head of row r.  A workgroup forms the angles of its rows once, in LDS:
-// the product of two floats is exact in 64 bits, so is its reduction to
-// [-1/2, 1/2] revolutions to about |t| 2^-53, and only that remainder is
-// rounded to fp32 before sin and cos -- a far coordinate costs no accuracy.
+// the product of two floats is exact in 64 bits, so is its reduction to quarters
+// of a revolution and a remainder of at most an eighth to about |t| 2^-53, and
+// only that remainder is rounded to fp32 before its sine and cosine -- a far
+// coordinate costs no accuracy.
 // Then every head's pairs are read, turned in fp32 and written, 16 bytes at
 // a time where the layout allows it.
 //
@@ -34,6 +35,16 @@ struct RotArgs {
     int end[MESORASI_MAX_AXES];      // first pair after each axis' section
     int copy;                        // the channels past the pairs have to be copied
 };
+
+// Sine and cosine of |x| <= pi / 4, from their power series: the terms left out
+// are below x 2e-9 and 2e-10.
+__device__ __forceinline__ void rot_sincos(float x, float& s, float& c) {
+    const float z = x * x;
+    const float p = fmaf(fmaf(fmaf(1.0f / 362880, z, -1.0f / 5040), z, 1.0f / 120), z, -1.0f / 6);
+    const float q = fmaf(fmaf(fmaf(-1.0f / 3628800, z, 1.0f / 40320), z, -1.0f / 720), z, 1.0f / 24);
+    s = fmaf(x * z, p, x);
+    c = fmaf(z, fmaf(z, q, -0.5f), 1.0f);
+}
 
 __device__ __forceinline__ float rot_load(const float* p) { return *p; }
 __device__ __forceinline__ float rot_load(const uint16_t* p) { return bf16_to_f32(*p); }
@@ -77,10 +88,12 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a) {
 #pragma unroll
         for (int k = 0; k < MESORASI_MAX_AXES - 1; ++k) ax += j >= a.end[k];
         const double rev = (double)a.pos[(r0 + r) * a.ldp + ax] * (double)a.freq[j] * 0.15915494309189533577;
-        const float h = (float)(rev - rint(rev));
+        const double quarters = rint(4.0 * rev);
+        const int q = (int)(quarters - 4.0 * rint(0.25 * quarters)) & 3;
         float s, c;
-        sincospif(2.0f * h, &s, &c);
-        ang[i] = make_float2(c, s);
+        rot_sincos((float)((rev - 0.25 * quarters) * 6.28318530717958647693), s, c);
+        const float x = q & 1 ? s : c, y = q & 1 ? c : s;        // turned by q quarters
+        ang[i] = make_float2(q == 1 || q == 2 ? -x : x, q >= 2 ? -y : y);
     }
     __syncthreads();
     const int nv = a.P / VEC;                                       // vectors of pairs of a head

@@ -962,3 +962,34 @@ def test_attention_shared_mask(gpu, dtype, Nq, Nk):
     got = ops.cross_attention(q, k, v, k_mask=mask)
     within(got, *_ref_and_bound(q, k, v, k_mask=mask))
     assert torch.equal(got, ops.cross_attention(q, k, v, k_mask=mask.contiguous()))
+
+
+def test_rotary_precision(gpu):
+    """fp32 over many angles, in the 2-norm: the remainder's rounding (at most
+    half a unit of pi / 4, uniform: 1.4e-8), sin and cos to a unit (3.4e-8), products
+    (half a unit of each, 1.2e-8 of the pair) and their sum (1.7e-8) add up to
+    4.3e-8 as independent errors."""
+    g = gen(42)
+    x, pos = randn(g, 20000, 4, 64), randn(g, 20000, 3) * 25
+    p = ops.RotaryParams([10, 10, 12], base=1000.0, scale=20.0)
+    y, _ = rotary_ref(x, pos, p.sections, p.freq, False)
+    err = float((ops.rotary(x, pos, p).double() - y).norm() / y.norm())
+    print("normwise error", err)
+    assert err <= 4.8e-8
+
+
+def test_rotary_quarter_turns(gpu):
+    """Angles at and around every eighth of a turn, of either sign, small and
+    large, and angles that are not finite."""
+    g = gen(43)
+    eighth = torch.arange(-64, 65, dtype=torch.float64, device="cuda") / 8
+    turn = torch.cat([eighth * 2 * math.pi, (eighth + 4096) * 2 * math.pi]).float()
+    pos = torch.cat([turn, torch.nextafter(turn, torch.full_like(turn, math.inf)),
+                     torch.nextafter(turn, torch.full_like(turn, -math.inf)), -turn])[:, None]
+    x = randn(g, pos.shape[0], 3, 6)
+    p = ops.RotaryParams([3], freq=torch.tensor([1.0, -0.5, 3.0]))
+    y, size = rotary_ref(x, pos, [3], p.freq, False)
+    within(ops.rotary(x, pos, p), y, size * 2.0 ** -21 + 1e-30)
+    pos[5], pos[6], pos[7] = math.inf, math.nan, 3e38
+    z = ops.rotary(x, pos, p)
+    assert bool(torch.isnan(z[5:7]).all()) and bool(torch.isfinite(z[7:]).all())
