@@ -654,7 +654,7 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  * are accumulated in fp32.  The bf16 form takes the weights p to their product
  * with v in 15 bits for few rows, rounded to bf16 for many; the fp32 form keeps
  * fp32 precision throughout (v below fp32's normal range may count as 0).
- * Scores past fp32's range are infinite: a source of score
+ * Scores (scaled or not) past fp32's range are infinite: a source of score
  * -infinity weighs 0, one of +infinity or NaN makes its queries NaN.  The sums
  * of 256 |v| over a query's valid sources have to stay within fp32's range.
  *   q [B, Nq, Hq, D], k and v [B, Nk, Hkv, D], o [B, Nq, Hq, D], all of dtype
@@ -674,7 +674,8 @@ int mesorasi_rotary(const void* x, int64_t ld_x, int32_t dtype, int64_t rows, in
  * Errors: EINVAL for NULL q/k/v/o, sizes < 0, Hq < 1, Hkv < 1,
  *         Hq % Hkv != 0, D < 1, a negative stride, an output stride < D (over
  *         more than one cloud, point or head), mask_ld < Nk and not 0 with a
- *         mask and more than one cloud, a scale that is not finite, a misaligned ws, o
+ *         mask and more than one cloud, a scale that is not finite (times
+ *         log2(e), in fp32), a misaligned ws, o
  *         that overlaps q, k or v;  EUNSUPPORTED for an unknown dtype,
  *         D > MESORASI_MAX_D_ATTN, Nq (Hq / Hkv) or Nk > 2^31 - 1024, or more
  *         work than one launch holds;  EWORKSPACE when ws is too small.

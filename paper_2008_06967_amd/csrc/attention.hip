@@ -97,6 +97,15 @@ __device__ __forceinline__ float at_other_half(float v, float& lo) {
     return __uint_as_float(r[1]);
 }
 
+// A query's sum of weights from its two lanes'.  Where its reference is
+// +infinity (the largest score times the scale passes fp32's range) the weights
+// are not defined, though exp2 of differences to it gives 0.
+__device__ __forceinline__ float at_weights(float l, float m) {
+    float lo;
+    const float hi = at_other_half(l, lo);
+    return m == INFINITY ? NAN : lo + hi;
+}
+
 __device__ __forceinline__ uint32_t at_pack(float a, float b) {
     bf16x2 v;
     v[0] = static_cast<__bf16>(a);
@@ -455,11 +464,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
 
     // the two lanes of a query join their sums
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        float lo;
-        const float hi = at_other_half(l[qb], lo);
-        l[qb] = lo + hi;
-    }
+    for (int qb = 0; qb < QB; ++qb) l[qb] = at_weights(l[qb], m[qb]);
     if constexpr (KS) {
         constexpr int Dp = 32 * DB;
         // the waves join: [wave][d][32 rows] sums, then their maxima and sums
@@ -671,12 +676,7 @@ struct AtRows {
                 for (int r = 0; r < 16; ++r) oacc[d][r] *= f;
         }
     }
-    // the two lanes of a query join their sums of weights
-    __device__ __forceinline__ void join_halves() {
-        float lo;
-        const float hi = at_other_half(l, lo);
-        l = lo + hi;
-    }
+    __device__ __forceinline__ void join_halves() { l = at_weights(l, m); }
     // a row without a weight is 0, whatever its sums hold
     template <bool GEN>
     __device__ __forceinline__ void write(const AttnArgs& a, const AtPlace& p, int row, int half) const {
@@ -1156,10 +1156,7 @@ __global__ __launch_bounds__(kAtThreads, (DQ * RB > 2 ? 1 : 2)) void attention_f
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
         const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[j]), __float_as_uint(l[j]), false, false);
-        l[j] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-        float lo;
-        const float hi = at_other_half(l[j], lo);
-        l[j] = lo + hi;
+        l[j] = at_weights(__uint_as_float(x[0]) + __uint_as_float(x[1]), m[j]);
 #pragma unroll
         for (int q = 0; q < DQ; ++q)
 #pragma unroll
@@ -1389,7 +1386,7 @@ extern "C" int mesorasi_cross_attention(const void* q, int64_t q_bs, int64_t q_l
     MESO_REQUIRE((B <= 1 || o_bs >= D) && (Nq <= 1 || o_ld >= D) && (Hq <= 1 || o_hs >= D), MESORASI_EINVAL,
                  "mesorasi_cross_attention: an output stride < D");
     MESO_REQUIRE(!k_mask || B <= 1 || mask_ld == 0 || mask_ld >= Nk, MESORASI_EINVAL, "mesorasi_cross_attention: mask_ld < Nk");
-    MESO_REQUIRE(std::isfinite(scale), MESORASI_EINVAL, "mesorasi_cross_attention: scale = %g", (double)scale);
+    MESO_REQUIRE(std::isfinite(scale * 1.4426951f), MESORASI_EINVAL, "mesorasi_cross_attention: scale = %g", (double)scale);
     MESO_REQUIRE(dtype == MESORASI_F32 || dtype == MESORASI_BF16, MESORASI_EUNSUPPORTED,
                  "mesorasi_cross_attention: dtype %d", dtype);
     MESO_REQUIRE(D <= MESORASI_MAX_D_ATTN, MESORASI_EUNSUPPORTED, "mesorasi_cross_attention: D = %d", D);

@@ -463,6 +463,7 @@ def test_cross_attention_validation_and_workspace():
                 dict(vs=(2048, 128, -64)), dict(os=(1024, 63, 64)), dict(os=(1024, 256, 63)), dict(os=(0, 256, 64)),
                 dict(mask=FAKE, mld=15), dict(scale=float("inf")), dict(scale=float("nan"))):
         assert st(f, *args(**bad)) == _lib.EINVAL, bad
+    assert st(f, *args(scale=3e38, o=ctypes.c_void_p(0x100000))) == _lib.EINVAL       # times log2(e)
     for bad in (dict(dt=2), dict(D=129, os=(9999, 999, 199)), dict(Nk=1 << 31), dict(Nq=1 << 30)):
         assert st(f, *args(**bad)) == _lib.EUNSUPPORTED, bad
     assert st(f, *args(q=NULL, o=NULL, B=0)) == _lib.OK

@@ -993,3 +993,18 @@ def test_rotary_quarter_turns(gpu):
     pos[5], pos[6], pos[7] = math.inf, math.nan, 3e38
     z = ops.rotary(x, pos, p)
     assert bool(torch.isnan(z[5:7]).all()) and bool(torch.isfinite(z[7:]).all())
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("Nq,Nk", [(2, 40), (2, 2000), (70, 130), (200, 90), (3000, 65)])
+def test_attention_scaled_scores_past_the_range(gpu, dtype, Nq, Nk):
+    """Scores that are finite until they are scaled: -infinity weighs nothing,
+    +infinity leaves no weights defined, and is no 0."""
+    g = gen(44)
+    q, k, v = (randn(g, 2, n, h, 48, dtype=dtype) for n, h in ((Nq, 8), (Nk, 4), (Nk, 4)))
+    q, k = q.abs() + 0.5, -(k.abs() + 0.5)
+    k[1, Nk // 2] *= -1.0                            # the second cloud has one source of positive scores
+    got = ops.cross_attention(q, k, v, scale=1e38)
+    assert bool((got[0] == 0).all()) and bool(torch.isnan(got[1]).all())
+    got = ops.cross_attention(q, k, v, scale=-1e38)
+    assert bool(torch.isnan(got).all())
