@@ -1,7 +1,8 @@
 // Cross attention to another set of points: o_i = sum_j p_ij v_j / sum_j p_ij,
 // p_ij = exp(s_ij - m_i), s_ij = scale q_i . k_j.
 //
-// One pass over the sources with a running reference m_i and sum: where a
+// One pass over the sources with a running reference m_i and sum (the online
+// normalizer calculation of Milakov and Gimelshein, 2018): where a
 // later score passes m_i by 8 (in powers of two) what was summed is scaled
 // down, otherwise m_i stays, so that the weights are at most 256 and most
 // tiles rescale nothing.  The queries of all heads that share a source head
@@ -16,10 +17,10 @@
 // Bounds.  Many rows: 4 D operations a pair on the matrix cores and the
 // weights on the vector units, which do not overlap whole.  4 x 16384 queries
 // over 4096 sources, 8 heads on 2, bf16: 1.10 ms, 1000 TFLOP/s at 128 channels
-// (matrix cores busy 46 %, 6.6 vector instructions counted a weight), 584 us,
-// 940 at 64 (41 %, 4.9), 396 us, 694 at 32; a large bf16 library product
-// reaches 1400.  Few rows: one read of K and V (8 x 1 query over 16384 sources,
-// 8 heads of 128: 188 us, 5.7 TB/s in fp32; 105 us, 5.1 TB/s in bf16).
+// (matrix cores busy 46 %, 7 vector instructions counted a weight), 580 us,
+// 948 at 64 (41 %, 5), 392 us, 702 at 32; a large bf16 library product reaches
+// 1400.  Few rows: one read of K and V (8 x 1 query over 16384 sources, 8 heads
+// of 128: 187 us, 5.7 TB/s in fp32; 107 us, 5.0 TB/s in bf16).
 #include <algorithm>
 #include <cmath>
 
@@ -195,8 +196,8 @@ __device__ __forceinline__ void at_write_part(const AttnArgs& a, int64_t pr, con
 //
 // Where the waves share rows the weights are kept in two bf16 parts, to 2^-15 of
 // each, and V is multiplied by both: such calls wait for memory or for their
-// few tiles (8 x 1 query over 16384 sources of 128 channels 105 us either way,
-// 1 x 1024 over 1024 of 64 10.8 -> 12.4).  The first part is rounded down and
+// few tiles (8 x 1 query over 16384 sources of 128 channels 106 us either way,
+// 1 x 1024 over 1024 of 64 10.8 -> 12.0).  The first part is rounded down and
 // the second above 0, so that an infinite v meets no 0 and no other sign.  With rows of their own they are
 // rounded to bf16, 2^-8 of each, whose errors average out over a row's sources
 // to about the output's own rounding: a second part costs what it adds to the
@@ -564,8 +565,8 @@ __device__ __forceinline__ f32x16 at_mfma6(const bf16x8 (&a)[3], const bf16x8 (&
 // instruction's 157.  K and V are split once a tile, on their way to LDS (the
 // next tile's rows wait in registers); Q once, the weights where they form.
 // Four waves with 32 rows of their own.  4 x 4096 queries over 1024 sources, 8
-// heads of 64: 185 us, 185 TFLOP/s, matrix cores busy 50 %; of 128: 457 us, 150,
-// busy 35 %, one wave a SIMD.
+// heads of 64: 181 us, 190 TFLOP/s, matrix cores busy 52 %; of 128: 443 us, 155,
+// busy 37 %, one wave a SIMD.
 //
 // Values that the parts do not hold show in the results.  An infinity or a huge
 // value in k, or products past fp32's range with parts of either sign, give NaN
@@ -1248,16 +1249,16 @@ AttnPlan plan_attention(int64_t B, int64_t Nq, int64_t Nk, int Hq, int Hkv, int 
     p.Dp = (D + 31) / 32 * 32;
     p.splits = 1;
     p.rb = 0;
-    // Parts of 128 sources and up, and the launch that joins them, past 512 sources (2 x 12 heads over 722, fp32: 8.9 us
-    // in parts of 128, 10.5 of 256, 12.1 of 512; 3 x 12 queries over 486, bf16: 7.3 us whole, 8.5 in parts of 128).
+    // Parts of 128 sources and up, and the launch that joins them, past 512 sources (2 x 12 heads of 64 over 722, fp32:
+    // 10.1 us in parts of 128, 12.1 of 256, 14.3 of 512; 3 x 12 queries over 486, bf16: 9.1 us whole, 9.9 in parts of 128).
     auto splits = [&](int64_t wg) {
         return Nk <= 512 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kAtMaxSplits / wg, ceil_div(Nk, 128)));
     };
-    // Two blocks a wave read the sources' operands half as often (64 channels: 585 -> 564 us for 4 x 16384 over 4096, 8
+    // Two blocks a wave read the sources' operands half as often (64 channels: 652 -> 608 us for 4 x 16384 over 4096, 8
     // heads) but above 64 channels leave one wave a SIMD (128: 1080 -> 1260 us).  Below a workgroup for most compute
-    // units, waves that share 32 rows and split the sources finish sooner (1 x 1024 over 1024, 8 heads of 64: 11 us
+    // units, waves that share 32 rows and split the sources finish sooner (1 x 1024 over 1024, 8 heads of 64: 12 us
     // instead of 22); in fp32, whose shared form is the slower instruction, only for few rows (4 x 349 over 10357, 4
-    // heads on 2, of 24: 79 us with rows of their own, 235 shared).  Up to 32 rows, one shared tile, share it however many
+    // heads on 2, of 24: 74 us with rows of their own, 229 shared).  Up to 32 rows, one shared tile, share it however many
     // clouds and heads there are: three waves of four would have no rows (32 x 1 over 4096, 8 heads of 128: fp32 417 us
     // with rows of their own, 179 shared, bf16 104 and 102; 32 x 32 over 2048, 8 heads of 64: 98 and 59, 36 and 26; the
     // other way about 64 x 1 over 1024 of 128 in bf16, 46 and 50; and past 32 rows fp32 64 x 64 over 257 of 32, 22 and 32).

@@ -170,7 +170,8 @@ __device__ __forceinline__ int wave_max_i32(int v) {
     return __builtin_amdgcn_readlane(v, 63);
 }
 
-// Division of 0 <= n < 2^31 by a fixed d >= 1: with l = ceil(log2 d) and M =
+// Division of 0 <= n < 2^31 by a fixed d >= 1 (Granlund and Montgomery, Division
+// by invariant integers using multiplication, 1994): with l = ceil(log2 d) and M =
 // ceil(2^(32 + l) / d), n / d is n M / 2^(32 + l) rounded down; M - 2^32 is kept.
 struct FastDiv {
     uint32_t d, m, l;

@@ -10,13 +10,13 @@
 // Two forms.  Where the rows of a run of whole groups fit the registers of
 // one workgroup, it reads them once, and one launch does all.  Otherwise one
 // launch forms the parts of chunks of rows and another joins them and
-// writes; its writes pass the caches by, which leaves them to x (140 us
-// instead of 168 for 16 x 16384 x 256 in fp32, gelu, the same x repeated).
+// writes; its writes pass the caches by, which leaves them to x (138 us
+// instead of 167 for 16 x 16384 x 256 in fp32, gelu, the same x repeated).
 //
 // Bound: one read and one write of HBM, and a second read where x is larger
-// than the caches (16 x 16384 x 256 fp32: 43 + 101 us, 6.2 and 5.3 TB/s).  The
+// than the caches (16 x 16384 x 256 fp32: 43 + 100 us, 6.3 and 5.4 TB/s).  The
 // small form is bound by its chain of loads, two sums over the workgroup and
-// stores (16 x 1023 x 192 bf16: 12.8 us, 128 x 128: 5.2).
+// stores (16 x 1023 x 192 bf16: 12.9 us, 128 x 128: 5.3).
 #include <algorithm>
 #include <cmath>
 
@@ -29,7 +29,7 @@ namespace {
 constexpr int kGnThreads = 256;      // of the two-launch form
 constexpr int kGnOneThreads = 512;   // of the one-launch form
 constexpr int kGnKeep = 16;          // vectors of a thread in the one-launch form, at most
-constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit (2048: 154 us for 135)
+constexpr int kGnBlocks = 1024;      // workgroups of the two-launch form: four a compute unit (2048: 157 us for 136)
 
 template <typename T, int N>
 struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) GnVec {
@@ -662,7 +662,7 @@ GnPlan plan_group_norm(int64_t B, int64_t N, int C, int G, int vec) {
     }
     const int64_t slots = std::max<int64_t>(1, kGnThreads / ceil_div(std::min<int64_t>(p.slab, C), vec));
     // Every workgroup of the second launch joins all chunks of its cloud, 16 parts a thread at most: 256 chunks for 8
-    // groups (1 x 65536 x 64: 15 us, with 128 20), 128 for 32 (1 x 16384 x 256: 25 us, with 256 30).  A thread's chain
+    // groups (1 x 65536 x 64: 16 us, with 128 20), 128 for 32 (1 x 16384 x 256: 26 us, with 256 31).  A thread's chain
     // of sums stays within 128 rows; at least 8 rows a thread.
     const int64_t most_chunks = std::max<int64_t>(64, std::min<int64_t>(256, 4096 / std::max(1, p.slab / c)));
     const int64_t want = std::min(most_chunks, std::max<int64_t>(1, kGnBlocks / std::max<int64_t>(1, B * p.slabs)));

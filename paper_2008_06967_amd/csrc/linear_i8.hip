@@ -4,13 +4,13 @@
 // Float rows are first brought to 8 bits (quantize_i8_kernel), or, where at
 // most 16 rows of at most 2048 columns come, in the product's registers.
 //
-// Measured.  The large product (16384 x 4096 -> 4096, 8-bit rows): 269 us, 2040
-// TOP/s, where the library's int8 product without scales takes 244 us, 2250;
-// at 8192 x 8192 -> 8192 2270 against 2480.  The matrix cores are busy 49 % of
+// Measured.  The large product (16384 x 4096 -> 4096, 8-bit rows): 270 us, 2040
+// TOP/s, where the library's int8 product without scales takes 247 us, 2220;
+// at 8192 x 8192 -> 8192 2270 against 2470.  The matrix cores are busy 50 % of
 // it and L2 serves 2.1 GB of tiles at 8 TB/s, so neither alone bounds it; what
 // takes the rest was not isolated.  16368 x 320 -> 256 from fp32: 16 us for the
 // 7 of its bytes, two launches and the 8-bit rows' round trip.  Few rows: the
-// latency of one chain of loads (13 x 1024 -> 512: 2.9 us from 8-bit rows, 6.1
+// latency of one chain of loads (13 x 1024 -> 512: 3.0 us from 8-bit rows, 6.0
 // from fp32).
 #include <algorithm>
 
@@ -83,8 +83,8 @@ __device__ __forceinline__ void qu_store(int8_t* q, const float (&f)[N], const Q
 // LPR lanes per row, 16 bytes of a row (of any alignment) at a time; the first
 // kQuKeep vectors of a lane stay in registers between the maximum and the
 // rounding, longer rows are read again.  Bound: one read of x and one write
-// of q (16384 x 4096 bf16: 45 us, 4.5 TB/s in a
-// trace; 32 us repeated on the same rows, which the caches then hold in part).
+// of q (16384 x 4096 bf16: 45 us, 4.5 TB/s
+// between products; 32 us repeated on the same rows, which the caches then hold in part).
 template <typename T, int LPR>
 __global__ __launch_bounds__(kQuThreads) void quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows,
                                                                  int C, int8_t* __restrict__ q, int64_t ldq,
