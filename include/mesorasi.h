@@ -531,8 +531,10 @@ int mesorasi_count_out_of_range(const int32_t* idx, int64_t n, int32_t bound, in
  * points n < len_b of cloud b
  *   mu = mean x, var = mean (x - mu)^2              (per cloud and group)
  *   y  = act((x - mu) / sqrt(var + eps) * gamma + beta)
- * with the statistics in fp32 or more.  Rows n >= len_b are not read and
- * are written as 0.
+ * with the statistics in fp32 or more: the mean to twice fp32's bits, so that
+ * values far from the others cost these no accuracy; a group's sum of (x - mu)^2
+ * has to stay within fp32's range.  Rows n >= len_b are not read and are written
+ * as 0.
  *   x     [B, N, ld_x] of x_dtype (F32 or BF16), first C columns used
  *   lens  [B] int32 or NULL (all N); a value outside [0, N] is taken as the
  *         nearest of the two

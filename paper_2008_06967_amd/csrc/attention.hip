@@ -198,11 +198,11 @@ __device__ __forceinline__ void at_write_part(const AttnArgs& a, int64_t pr, con
 // each, and V is multiplied by both: such calls wait for memory or for their
 // few tiles (8 x 1 query over 16384 sources of 128 channels 106 us either way,
 // 1 x 1024 over 1024 of 64 10.8 -> 12.0).  The first part is rounded down and
-// the second above 0, so that an infinite v meets no 0 and no other sign.  With rows of their own they are
-// rounded to bf16, 2^-8 of each, whose errors average out over a row's sources
-// to about the output's own rounding: a second part costs what it adds to the
-// matrix cores and the vector units (4 x 16384 over 4096, 8 heads on 2: 1120 ->
-// 1530 us at 128 channels, 591 -> 877 at 64).
+// the second above 0, so that an infinite v meets no 0 and no other sign.  With
+// rows of their own they are rounded to bf16, 2^-8 of each, whose errors average
+// out over a row's sources to about the output's own rounding: a second part
+// costs what it adds to the matrix cores and the vector units (4 x 16384 over
+// 4096, 8 heads on 2: 1120 -> 1530 us at 128 channels, 591 -> 877 at 64).
 template <int DB, int QB, bool KS, bool GEN>
 __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs a) {
     constexpr int CH = DB == 1 ? 4 : DB == 2 ? 8 : 16;       // 16-byte chunks of a row in LDS
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void attention_bf16_kernel(AttnArgs 
             }
         }
         // weights: the reference m of a query moves when its maximum passes it by 8 (a factor of 256)
-        uint32_t pk[QB][NB][8], pl[QB][NB][8];           // pl: what the rounding left over (KS)
+        uint32_t pk[QB][NB][8], pl[QB][NB][8];           // pl: the second parts (KS)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             float mx = -INFINITY;
@@ -712,9 +712,9 @@ struct AtRows {
 // A wave's queries in `again` on v_mfma_f32_32x32x2_f32, which takes any value:
 // a lane supplies row or column lane % 32 and k = lane / 32.  Scores: channels
 // 8 i + 4 (lane / 32) + e are step (i, e).  Outputs: step r takes the sources of
-// the lane's own weights.  Block, thread and arguments pass through an empty asm, so
-// that the kernel before it keeps none of this in registers (with it 4 to 8 %
-// slower).
+// the lane's own weights.  Block, thread and the kernel's arguments (its only
+// parameter) are taken through an empty asm, so that the kernel before it keeps
+// none of this in registers (it was 4 to 8 % slower with them).
 template <int DB, bool GEN>
 __device__ __forceinline__ void attention_f32_plain(int block, int tid, uint32_t again, char* lds) {
     using P = AtF32<DB>;
