@@ -864,8 +864,10 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     layout transposed, the filled part of a longer buffer).  k_len [B] int32:
     sources from k_len[b] on are not valid; k_mask [B, Nk] bool (its
     clouds may share one row): only the True ones are.  A query without a valid source gives 0.  scale: 1 / sqrt(D)
-    unless given.  out: like q (its strides may differ); it may not overlap q, k
-    or v, other columns of their rows aside."""
+    unless given.  bfloat16 rounds the weights to its 8 bits where there are many
+    rows (see the C header); float32 keeps float32's.  out: like q (its strides
+    may differ); it may not overlap q, k or v, other columns of their rows
+    aside."""
     qs, ks = q.shape, k.shape
     _require(len(qs) == 4 and len(ks) == 4 and v.shape == ks, "q must be [B, Nq, Hq, D], k and v [B, Nk, Hkv, D]")
     B, Nq, Hq, D = qs
